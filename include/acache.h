@@ -475,6 +475,74 @@ acache_status acache_linear(const acache_dims* dims, const void* a, const void* 
                             void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* ---------------------------------------------------------------------------
+ * An 8-bit KV cache: the pools of one layer held as e4m3 codes (1 sign, 4
+ * exponent, 3 significand bits, largest value 448, no infinity) with one
+ * scale for every block of `block` consecutive slots and KV head.  An entry's
+ * value is its code times its block's scale.  Scales are powers of two, so
+ * the product is exact in bf16 and fp32; a scale of 0 marks an empty block,
+ * whose slots read as zeros whatever their codes.  A new cache is made by
+ * setting both scale arrays to zero; the codes need no initial value.
+ * Clearing a block's scales empties it again, which a caller does when it
+ * gives the block's slots to another request (otherwise the block keeps the
+ * larger scale of its earlier entries until all of its slots are written by
+ * one call).  head_dim % 16 == 0; the 8-bit calls otherwise take the dims
+ * that acache_attention takes (of them they read n_heads, n_kv_heads,
+ * head_dim and dtype). */
+typedef struct {
+  void* k_codes;   /* [n_slots, ld] one byte each, a slot's row H_kv heads of head_dim (K after rotation) */
+  void* v_codes;   /* [n_slots, ld] */
+  float* k_scales; /* [ceil(n_slots / block), H_kv] */
+  float* v_scales; /* [ceil(n_slots / block), H_kv] */
+  int64_t ld;      /* >= H_kv * head_dim, multiple of 16 */
+  int64_t n_slots; /* < 2^31 */
+  int32_t block;   /* 16, 32, 64, 128 or 256 */
+} acache_quant_pool;
+
+/* acache_quant_store — acache_kv_scatter into an 8-bit cache: k_src row i and
+ * v_src row i (dims->dtype, [n, src_ld], H_kv * head_dim elements) become the
+ * values of slot dst_slots[i], rounded to nearest even.  With e the exponent
+ * of a block and head's scale and `need` the smallest exponent with
+ * |x| <= 448 * 2^need for every finite new element x of that block and head
+ * (within [-117, 119]; larger elements saturate):
+ *   - a block all of whose slots this call writes, or that was empty, takes
+ *     e = need; slots of an empty block that are not written get the value 0
+ *     (which they had);
+ *   - any other block takes the larger of its e and need, and where that
+ *     raises e, the entries it keeps are rounded to the new scale.
+ * An infinity or NaN is stored as NaN and does not raise the scale.  Of rows
+ * that name one slot the last is stored.  Rows whose slot is outside
+ * [0, n_slots) are skipped.  Untouched blocks keep every bit.  The result
+ * does not depend on the order of the work: identical inputs give identical
+ * bits.  ws: at least acache_quant_workspace_size(dims, 0, pool) bytes, no
+ * initial contents needed.  n == 0: no-op. */
+acache_status acache_quant_store(const acache_dims* dims, const acache_quant_pool* pool, const void* k_src,
+                                 const void* v_src, int64_t src_ld, int32_t n, const int32_t* dst_slots, void* ws,
+                                 size_t ws_bytes, hipStream_t stream);
+
+/* acache_quant_load — the values of slots[i], i < n, as rows of dims->dtype:
+ * k_dst and v_dst [n, dst_ld] (either may be NULL: not read back).  A slot
+ * outside [0, n_slots) gives a row of zeros.  n == 0: no-op. */
+acache_status acache_quant_load(const acache_dims* dims, const acache_quant_pool* pool, const int32_t* slots,
+                                int32_t n, void* k_dst, void* v_dst, int64_t dst_ld, hipStream_t stream);
+
+/* acache_quant_attention — acache_attention over an 8-bit cache: the same
+ * operation, layouts and ragged batch with K_j and V_j the cache's values
+ * (a slot outside [0, n_slots) is a key and a value of zeros, as there).
+ * bf16 only (ACACHE_ERR_UNSUPPORTED otherwise), n_slots * ld < 2^31.  Scales
+ * other than powers of two are read as the power of two at or below them.
+ * ws is optional: with acache_quant_workspace_size(dims, rows, pool) bytes
+ * the keys of calls with few rows are split over workgroups (fp32 partials,
+ * combined in a fixed order); with less, in fewer parts or none. */
+acache_status acache_quant_attention(const acache_dims* dims, const acache_ragged* rg, const void* q,
+                                     const int32_t* read_slots, const acache_quant_pool* pool, void* out, float* lse,
+                                     void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Workspace bytes for acache_quant_store into `pool` and for
+ * acache_quant_attention of up to max_rows rows over it.  Returns 0 for
+ * invalid dims or an invalid pool (its pointers are not looked at). */
+size_t acache_quant_workspace_size(const acache_dims* dims, int32_t max_rows, const acache_quant_pool* pool);
+
+/* ---------------------------------------------------------------------------
  * Measurement hook (benchmarks only).  While armed for kernel `kernel`,
  * every launch of that kernel by any entry point records starts[i] before
  * and stops[i] after it on the launch stream, i = *count, *count + 1, ...,

@@ -54,6 +54,12 @@ class Layout(ctypes.Structure):
                                               "shared_base", "private_base", "private_stride", "key_order")]
 
 
+class QuantPoolDesc(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("ld", ctypes.c_int64), ("n_slots", ctypes.c_int64),
+                ("block", ctypes.c_int32)]
+
+
 class Paging(ctypes.Structure):
     _fields_ = [("block_size", ctypes.c_int32), ("blocks_per_request", ctypes.c_int32),
                 ("shared_blocks", ctypes.c_void_p), ("private_blocks", ctypes.c_void_p)]
@@ -94,12 +100,20 @@ def _load():
         "acache_layer_schedule": [ctypes.POINTER(Dims), I32, PI, PI],
         "acache_linear": [ctypes.POINTER(Dims), P, P, P, I32, I32, I32, I32, P, SZ, P],
     }
+    QP = ctypes.POINTER(QuantPoolDesc)
+    sig.update({
+        "acache_quant_store": [ctypes.POINTER(Dims), QP, P, P, I64, I32, P, P, SZ, P],
+        "acache_quant_load": [ctypes.POINTER(Dims), QP, P, I32, P, P, I64, P],
+        "acache_quant_attention": [ctypes.POINTER(Dims), ctypes.POINTER(Ragged), P, P, QP, P, P, P, SZ, P],
+    })
     for name, args in sig.items():
         fn = getattr(lib, name)
         fn.argtypes = args
         fn.restype = ctypes.c_int32
     lib.acache_workspace_size.argtypes = [ctypes.POINTER(Dims), I32, I32, I32]
     lib.acache_workspace_size.restype = ctypes.c_size_t
+    lib.acache_quant_workspace_size.argtypes = [ctypes.POINTER(Dims), I32, QP]
+    lib.acache_quant_workspace_size.restype = ctypes.c_size_t
     lib.acache_status_string.argtypes = [ctypes.c_int32]
     lib.acache_status_string.restype = ctypes.c_char_p
     lib.acache_version.restype = ctypes.c_int32
@@ -489,6 +503,155 @@ def acache_threshold_commit(block: int, pick: torch.Tensor, conf: torch.Tensor, 
     _check("acache_threshold_commit", lib.acache_threshold_commit(
         batch, block, _ptr(pick), _ptr(conf), float(tau), _ptr(committed), _ptr(commit_pos), _ptr(ids),
         ids.numel(), _ptr(count), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------- 8-bit KV cache
+class QuantPool:
+    """One layer's 8-bit K and V: codes [n_slots, ld] (uint8, or
+    float8_e4m3fn) and scales [ceil(n_slots / block), H_kv] fp32, one power of
+    two for each block of consecutive slots and KV head (0: an empty block)."""
+
+    def __init__(self, k_codes: torch.Tensor, v_codes: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor,
+                 block: int):
+        for t in (k_codes, v_codes):
+            if t.dtype not in (torch.uint8, torch.float8_e4m3fn) or t.dim() != 2 or t.stride(1) != 1:
+                raise TypeError("codes must be uint8 or float8_e4m3fn [n_slots, ld] tensors with contiguous rows")
+        if k_codes.shape != v_codes.shape or k_codes.stride(0) != v_codes.stride(0):
+            raise ValueError("k_codes and v_codes must have the same shape and row stride")
+        n_blocks = -(-k_codes.shape[0] // block) if block > 0 else 0
+        for t in (k_scales, v_scales):
+            if t.dtype != torch.float32 or t.dim() != 2 or not t.is_contiguous():
+                raise TypeError("scales must be contiguous float32 [n_blocks, H_kv] tensors")
+            if t.shape[0] != n_blocks or t.shape != k_scales.shape:
+                raise ValueError("scales must hold ceil(n_slots / block) rows of H_kv values")
+        if any(t.device != k_codes.device for t in (v_codes, k_scales, v_scales)):
+            raise ValueError("codes and scales must be on one device")
+        self.k_codes, self.v_codes, self.k_scales, self.v_scales = k_codes, v_codes, k_scales, v_scales
+        self.block = block
+        # a row's addressable width: past its last element a strided view's row belongs to someone else
+        self.width, self.heads, self.device = k_codes.shape[1], k_scales.shape[1], k_codes.device
+        ld = k_codes.stride(0) if k_codes.shape[0] > 1 else k_codes.shape[1]
+        self.desc = QuantPoolDesc(k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(),
+                                  ld, k_codes.shape[0], block)
+        self.ref = ctypes.byref(self.desc)
+
+    def clear(self, slots: Optional[slice] = None):
+        """Empties every block (slots None) or those that lie wholly in the
+        given slots: their entries read as zeros."""
+        if slots is None:
+            first, last = 0, self.k_scales.shape[0]
+        else:
+            start, stop, step = slots.indices(self.k_codes.shape[0])
+            if step != 1:
+                raise ValueError("slots must be a range without a step")
+            first, last = -(-start // self.block), stop // self.block
+            if stop == self.k_codes.shape[0]:
+                last = self.k_scales.shape[0]
+        for t in (self.k_scales, self.v_scales):
+            t[first:max(first, last)].zero_()
+
+
+def quant_pool(dims: Dims, n_slots: int, block: int = 64, device="cuda") -> QuantPool:
+    """An empty 8-bit cache of n_slots slots."""
+    row = dims.n_kv_heads * dims.head_dim
+    codes = [torch.empty((n_slots, row), dtype=torch.uint8, device=device) for _ in range(2)]
+    scales = [torch.zeros((-(-n_slots // block), dims.n_kv_heads), dtype=torch.float32, device=device)
+              for _ in range(2)]
+    return QuantPool(*codes, *scales, block)
+
+
+def acache_quant_workspace_size(dims: Dims, max_rows: int, pool: QuantPool) -> int:
+    n = lib.acache_quant_workspace_size(ctypes.byref(dims), max_rows, pool.ref)
+    if n == 0:
+        raise AcacheError("acache_quant_workspace_size", 2, "invalid dims or pool")
+    return n
+
+
+def quant_workspace(dims: Dims, max_rows: int, pool: QuantPool) -> torch.Tensor:
+    """Workspace for acache_quant_store into `pool` and acache_quant_attention
+    of up to max_rows rows over it."""
+    return torch.empty(acache_quant_workspace_size(dims, max_rows, pool), dtype=torch.uint8, device=pool.device)
+
+
+def _quant_check(dims: Dims, pool: QuantPool, *tensors):
+    """The pool fits dims, and everything is on the current device."""
+    if pool.heads != dims.n_kv_heads or pool.width < dims.n_kv_heads * dims.head_dim:
+        raise ValueError("the pool's rows do not hold dims.n_kv_heads heads of dims.head_dim")
+    if pool.device.type != "cuda" or pool.device.index != torch.cuda.current_device():
+        raise ValueError(f"the pool is on {pool.device}, not on the current device")
+    for t in tensors:
+        if t is not None and t.device != pool.device:
+            raise ValueError(f"a tensor is on {t.device} and the pool on {pool.device}")
+
+
+def _quant_rows(dims: Dims, t: torch.Tensor, n: int, name: str):
+    if (t.dtype != torch_dtype(dims) or t.dim() != 2 or t.shape[0] != n
+            or t.shape[1] != dims.n_kv_heads * dims.head_dim or t.stride(1) != 1):
+        raise TypeError(f"{name} must be [{n}, n_kv_heads * head_dim] of dims' type with contiguous rows")
+
+
+def acache_quant_store(dims: Dims, pool: QuantPool, k_src: torch.Tensor, v_src: torch.Tensor,
+                       dst_slots: torch.Tensor, ws: Optional[torch.Tensor] = None, stream=None):
+    """Rows i of K and V become the values of slots dst_slots[i]."""
+    _dev_i32(dst_slots, "dst_slots")
+    n = dst_slots.numel()
+    for t, name in ((k_src, "k_src"), (v_src, "v_src")):
+        _quant_rows(dims, t, n, name)
+    if n > 1 and k_src.stride(0) != v_src.stride(0):
+        raise ValueError("k_src and v_src must have the same row stride")
+    if ws is None:
+        ws = quant_workspace(dims, 0, pool)
+    _quant_check(dims, pool, k_src, v_src, dst_slots, ws)
+    ld = k_src.stride(0) if n > 1 else k_src.shape[1]
+    _check("acache_quant_store", lib.acache_quant_store(
+        ctypes.byref(dims), pool.ref, k_src.data_ptr(), v_src.data_ptr(), ld, n, dst_slots.data_ptr(), ws.data_ptr(),
+        ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def acache_quant_load(dims: Dims, pool: QuantPool, slots: torch.Tensor, k_out: Optional[torch.Tensor] = None,
+                      v_out: Optional[torch.Tensor] = None, stream=None):
+    """(k, v) rows [n, n_kv_heads * head_dim] of the slots' values.  With
+    k_out or v_out given, only what is given is read back."""
+    _dev_i32(slots, "slots")
+    n = slots.numel()
+    if k_out is None and v_out is None:
+        k_out, v_out = (torch.empty((n, dims.n_kv_heads * dims.head_dim), dtype=torch_dtype(dims), device=slots.device)
+                        for _ in range(2))
+    given = [t for t in (k_out, v_out) if t is not None]
+    for t in given:
+        _quant_rows(dims, t, n, "k_out and v_out")
+    if n > 1 and given[0].stride(0) != given[-1].stride(0):
+        raise ValueError("k_out and v_out must have the same row stride")
+    _quant_check(dims, pool, slots, *given)
+    ld = given[0].stride(0) if n > 1 else given[0].shape[1]
+    _check("acache_quant_load", lib.acache_quant_load(
+        ctypes.byref(dims), pool.ref, slots.data_ptr(), n, _ptr(k_out), _ptr(v_out), ld, _stream(stream)))
+    return k_out, v_out
+
+
+def acache_quant_attention(dims: Dims, cu_rows, cu_keys, q: torch.Tensor, read_slots: torch.Tensor, pool: QuantPool,
+                           out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                           ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """acache_attention over an 8-bit cache.  ws (optional, from
+    quant_workspace): lets the keys of few rows be split over workgroups."""
+    _dev_i32(read_slots, "read_slots")
+    rg, keep = _ragged(cu_rows, cu_keys)
+    if out is None:
+        out = torch.empty_like(q)
+    rows, width = int(cu_rows[-1]), dims.n_heads * dims.head_dim
+    for t, name in ((q, "q"), (out, "out")):
+        if t.dtype != torch_dtype(dims) or t.numel() < rows * width or not t.is_contiguous():
+            raise TypeError(f"{name} must be a contiguous tensor of dims' type with [rows, n_heads * head_dim] values")
+    if read_slots.numel() < int(cu_keys[-1]):
+        raise ValueError("read_slots must hold cu_keys[-1] slots")
+    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous()
+                            or lse.numel() < rows * dims.n_heads):
+        raise TypeError("lse must be a contiguous float32 tensor of [rows, n_heads] values")
+    _quant_check(dims, pool, q, read_slots, out, lse, ws)
+    _check("acache_quant_attention", lib.acache_quant_attention(
+        ctypes.byref(dims), ctypes.byref(rg), q.data_ptr(), read_slots.data_ptr(), pool.ref, out.data_ptr(),
+        _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)))
+    return out
 
 
 # ---------------------------------------------------------------------------- measurement hook

@@ -916,4 +916,100 @@ acache_status acache_layer_decode(const acache_dims* dims, const acache_layer_we
   return run_out_mlp_bf16(dims, w, M, x, y, o, hb, part, stream);
 }
 
+// Host checks of an 8-bit cache's description, and the kernels' copy of it.
+static acache_status check_quant_pool(const acache_dims* dims, const acache_quant_pool* pool, QuantPool& out) {
+  acache_status st = check_dims(dims);
+  if (st != ACACHE_OK) return st;
+  CHECK(pool, ACACHE_ERR_NULL);
+  CHECK(dims->head_dim % 16 == 0, ACACHE_ERR_UNSUPPORTED);
+  CHECK(pool->ld >= (int64_t)dims->n_kv_heads * dims->head_dim && pool->n_slots >= 0, ACACHE_ERR_SHAPE);
+  CHECK(pool->n_slots < ((int64_t)1 << 31), ACACHE_ERR_SHAPE);
+  int shift = 4;
+  while (shift < 8 && (1 << shift) != pool->block) ++shift;
+  CHECK((1 << shift) == pool->block, ACACHE_ERR_UNSUPPORTED);
+  CHECK(pool->ld % 16 == 0, ACACHE_ERR_ALIGN);
+  out.codes[0] = pool->k_codes;
+  out.codes[1] = pool->v_codes;
+  out.scales[0] = pool->k_scales;
+  out.scales[1] = pool->v_scales;
+  out.ld = pool->ld;
+  out.n_slots = pool->n_slots;
+  out.shift = shift;
+  out.heads = dims->n_kv_heads;
+  out.head_dim = dims->head_dim;
+  return ACACHE_OK;
+}
+
+static acache_status check_quant_buffers(const QuantPool& p) {
+  CHECK(p.codes[0] && p.codes[1] && p.scales[0] && p.scales[1], ACACHE_ERR_NULL);
+  CHECK(aligned16(p.codes[0]) && aligned16(p.codes[1]), ACACHE_ERR_ALIGN);
+  return ACACHE_OK;
+}
+
+size_t acache_quant_workspace_size(const acache_dims* dims, int32_t max_rows, const acache_quant_pool* pool) {
+  QuantPool p;
+  if (check_quant_pool(dims, pool, p) != ACACHE_OK || max_rows < 0) return 0;
+  return align_up(std::max<size_t>(quant_map_bytes(p.n_slots, p.shift), 1));
+}
+
+acache_status acache_quant_store(const acache_dims* dims, const acache_quant_pool* pool, const void* k_src,
+                                 const void* v_src, int64_t src_ld, int32_t n, const int32_t* dst_slots, void* ws,
+                                 size_t ws_bytes, hipStream_t stream) {
+  QuantPool p;
+  acache_status st = check_quant_pool(dims, pool, p);
+  if (st != ACACHE_OK) return st;
+  CHECK(n >= 0, ACACHE_ERR_SHAPE);
+  if (n == 0) return ACACHE_OK;
+  CHECK(k_src && v_src && dst_slots, ACACHE_ERR_NULL);
+  st = check_quant_buffers(p);
+  if (st != ACACHE_OK) return st;
+  const int64_t es = (int64_t)elem_size(dims->dtype);
+  CHECK(src_ld >= (int64_t)p.heads * p.head_dim, ACACHE_ERR_SHAPE);
+  CHECK(aligned16(k_src) && aligned16(v_src) && (src_ld * es) % 16 == 0, ACACHE_ERR_ALIGN);
+  CHECK(p.heads <= 32767, ACACHE_ERR_UNSUPPORTED);  // K and V of every head are a grid dimension
+  CHECK(ws && ((uintptr_t)ws & 3u) == 0 && ws_bytes >= quant_map_bytes(p.n_slots, p.shift), ACACHE_ERR_WORKSPACE);
+  LAUNCH_T(ACACHE_K_SCATTER, stream,
+           launch_quant_store(dims->dtype, p, k_src, v_src, src_ld, n, dst_slots, (int32_t*)ws, stream));
+  return ACACHE_OK;
+}
+
+acache_status acache_quant_load(const acache_dims* dims, const acache_quant_pool* pool, const int32_t* slots,
+                                int32_t n, void* k_dst, void* v_dst, int64_t dst_ld, hipStream_t stream) {
+  QuantPool p;
+  acache_status st = check_quant_pool(dims, pool, p);
+  if (st != ACACHE_OK) return st;
+  CHECK(n >= 0, ACACHE_ERR_SHAPE);
+  if (n == 0 || (!k_dst && !v_dst)) return ACACHE_OK;
+  CHECK(slots, ACACHE_ERR_NULL);
+  st = check_quant_buffers(p);
+  if (st != ACACHE_OK) return st;
+  const int64_t es = (int64_t)elem_size(dims->dtype);
+  CHECK(dst_ld >= (int64_t)p.heads * p.head_dim, ACACHE_ERR_SHAPE);
+  CHECK(aligned16(k_dst) && aligned16(v_dst) && (dst_ld * es) % 16 == 0, ACACHE_ERR_ALIGN);
+  LAUNCH_T(ACACHE_K_GATHER, stream, launch_quant_load(dims->dtype, p, slots, n, k_dst, v_dst, dst_ld, stream));
+  return ACACHE_OK;
+}
+
+acache_status acache_quant_attention(const acache_dims* dims, const acache_ragged* rg, const void* q,
+                                     const int32_t* read_slots, const acache_quant_pool* pool, void* out, float* lse,
+                                     void* ws, size_t ws_bytes, hipStream_t stream) {
+  QuantPool p;
+  acache_status st = check_quant_pool(dims, pool, p);
+  if (st != ACACHE_OK) return st;
+  CHECK(dims->dtype == ACACHE_BF16, ACACHE_ERR_UNSUPPORTED);
+  Ragged r;
+  st = make_ragged(rg, r);
+  if (st != ACACHE_OK) return st;
+  if (r.cu_rows[r.batch] == 0) return ACACHE_OK;
+  CHECK(q && read_slots && out, ACACHE_ERR_NULL);
+  st = check_quant_buffers(p);
+  if (st != ACACHE_OK) return st;
+  CHECK(p.n_slots * p.ld < ((int64_t)1 << 31), ACACHE_ERR_UNSUPPORTED);  // 32-bit offsets
+  CHECK(aligned16(q) && aligned16(out), ACACHE_ERR_ALIGN);
+  CHECK(!ws || aligned16(ws), ACACHE_ERR_ALIGN);
+  LAUNCH_T(ACACHE_K_ATTENTION, stream,
+           launch_quant_attention(r, dims->n_heads, p, q, read_slots, out, lse, (float*)ws, ws ? ws_bytes : 0, stream));
+  return ACACHE_OK;
+}
+
 }  // extern "C"

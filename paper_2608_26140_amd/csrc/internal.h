@@ -144,6 +144,24 @@ hipError_t launch_score_fused_bf16(int batch, const int* cu_q, int H, int Hkv, c
                                    int64_t n_slots, const int32_t* affix_slots, int L, const float* row_lse,
                                    float* part, size_t part_bytes, int* rows_per_request, hipStream_t s);
 
+// ---- 8-bit KV cache (k_quant.hip, k_quant_attention.hip); K at index 0, V at 1
+struct QuantPool {
+  void* codes[2];    // [n_slots, ld] e4m3
+  float* scales[2];  // [blocks of 1 << shift slots, heads]
+  int64_t ld, n_slots;
+  int shift, heads, head_dim;
+};
+// Scratch of a store: for every slot the row written to it, for every block
+// its highest row (int32; no initial contents needed).
+size_t quant_map_bytes(int64_t n_slots, int shift);
+hipError_t launch_quant_store(acache_dtype dt, const QuantPool& p, const void* k, const void* v, int64_t src_ld, int n,
+                              const int32_t* slots, int32_t* map, hipStream_t s);
+// k or v may be null (not read back)
+hipError_t launch_quant_load(acache_dtype dt, const QuantPool& p, const int32_t* slots, int n, void* k, void* v,
+                             int64_t dst_ld, hipStream_t s);
+hipError_t launch_quant_attention(const Ragged& rg, int H, const QuantPool& p, const void* q, const int32_t* read_slots,
+                                  void* out, float* lse, float* part, size_t part_bytes, hipStream_t s);
+
 // ---- fp32 path (k_f32.hip)
 hipError_t launch_gemm_f32(const float* X, const float* W, float* C, int64_t ldc, int M, int N,
                            int K, int accumulate, hipStream_t s);
