@@ -949,7 +949,8 @@ static acache_status check_quant_buffers(const QuantPool& p) {
 size_t acache_quant_workspace_size(const acache_dims* dims, int32_t max_rows, const acache_quant_pool* pool) {
   QuantPool p;
   if (check_quant_pool(dims, pool, p) != ACACHE_OK || max_rows < 0) return 0;
-  return align_up(std::max<size_t>(quant_map_bytes(p.n_slots, p.shift), 1));
+  return align_up(std::max<size_t>({quant_map_bytes(p.n_slots, p.shift), 1,
+                                    quant_attention_part_bytes((int64_t)max_rows * dims->n_heads)}));
 }
 
 acache_status acache_quant_store(const acache_dims* dims, const acache_quant_pool* pool, const void* k_src,
