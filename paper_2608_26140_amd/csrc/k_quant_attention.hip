@@ -19,6 +19,8 @@
 //
 // With grouped heads the query heads of a KV head are further queries of the
 // same tile: a request's query v is row v mod rows of head g rep + v / rows.
+// Two kernels share the work (launch_quant_attention): 256 queries a
+// workgroup, or 32 with the keys dealt to its waves.
 #include <algorithm>
 #include <type_traits>
 
@@ -51,7 +53,9 @@ struct QAttnArgs {
   float* part_o;   // [splits][rows][H][128] unnormalised O (splits > 1)
   float* part_ml;  // [splits][rows][H][2] (running max in log2 units, sum)
   int H, rep, splits;
-  Ragged rg;       // tile_start: query tiles of a KV head
+  Ragged rg;       // tile_start: this launch's query tiles of a KV head
+  // this launch's queries of request b: v_lo[b] .. v_hi[b] - 1 of its rows * rep
+  int v_lo[kMaxBatch], v_hi[kMaxBatch];
 };
 
 // key (within a 32-key block) that S^T row i holds
@@ -84,19 +88,21 @@ __device__ __forceinline__ void convert16(u32x4 w, float scale, u32x4 (&v)[2]) {
   }
 }
 
-// The (KV head, request, query tile, key split) of a workgroup: KV heads
-// outermost and XCD-contiguous, so that workgroups that share keys share an L2.
+// The (KV head, request, query tile, key split) of a workgroup: an eighth of
+// the grid on each XCD, KV heads outermost, `side` of them next to each other.
 struct Unit {
   int g, b, tile, split;
 };
-__device__ __forceinline__ Unit unit_of(const Ragged& rg, int splits) {
+__device__ __forceinline__ Unit unit_of(const Ragged& rg, int splits, int side) {
   const int n_tiles = rg.tile_start[rg.batch];
   const int nb = gridDim.x, i = blockIdx.x;
   const int q8 = nb >> 3, r8 = nb & 7, x = i & 7;
   const int t = x * q8 + min(x, r8) + (i >> 3);
   Unit u;
-  u.g = t / (n_tiles * splits);
-  const int rem = t - u.g * n_tiles * splits;
+  const int group = t / (n_tiles * splits * side);
+  int rem = t - group * (n_tiles * splits * side);
+  u.g = group * side + rem % side;
+  rem /= side;
   u.tile = rem / splits;
   u.split = rem - u.tile * splits;
   int lo = 0, hi = rg.batch - 1;
@@ -170,24 +176,26 @@ __global__ __launch_bounds__(kWdThreads, 1) void quant_attention_wide_kernel(QAt
   __shared__ __attribute__((aligned(256))) char ks_ring[kWdAux * kAuxB];
   __shared__ __attribute__((aligned(256))) char vs_ring[kWdAux * kAuxB];
 
-  const Unit un = unit_of(a.rg, a.splits);
+  const Unit un = unit_of(a.rg, a.splits, (a.p.heads & 7) == 0 ? a.p.heads >> 3 : 1);
   const int g = un.g, b = un.b;
   const int tid = threadIdx.x, lane = tid & 63, hl = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int nr = a.rg.cu_rows[b + 1] - a.rg.cu_rows[b];
-  const int q0 = un.tile * kWdTileQ + wave * 32;
-  const bool live = q0 < nr * a.rep;  // wave-uniform: a wave without a query only copies and converts
+  const int q0 = a.v_lo[b] + un.tile * kWdTileQ + wave * 32;
+  const bool live = q0 < a.v_hi[b];  // wave-uniform: a wave without a query only copies and converts
   const int v = q0 + (lane & 31);
-  const bool q_ok = v < nr * a.rep;
+  const bool q_ok = v < a.v_hi[b];
   const int64_t pair = (int64_t)(a.rg.cu_rows[b] + (q_ok ? v % nr : 0)) * a.H + g * a.rep + (q_ok ? v / nr : 0);
   const int S = a.rg.cu_keys[b + 1] - a.rg.cu_keys[b];
   const int n_kt = (S + kTileK - 1) / kTileK;
   const int t_lo = (int)((int64_t)un.split * n_kt / a.splits), t_hi = (int)((int64_t)(un.split + 1) * n_kt / a.splits);
-  const int key_end = min(S, t_hi * kTileK);  // the workgroup's keys end here
+  const int key0 = t_lo * kTileK, n_keys = min(S, t_hi * kTileK) - key0;  // the workgroup's keys
+  const int n_t = t_hi - t_lo;
 
   bf16x8 qf[8];
   load_query(a.q + pair * kDh, q_ok, hl, qf);
 
+  const uint32_t n_slots = (uint32_t)a.p.n_slots;
   const uint32_t pool_b = (uint32_t)(a.p.n_slots * a.p.ld);  // < 2^31
   const uint32_t scale_b = (uint32_t)(((a.p.n_slots + (1 << a.p.shift) - 1) >> a.p.shift) * a.p.heads * 4);
   const rsrc_words kres = buffer_words(a.p.codes[0], pool_b), vres = buffer_words(a.p.codes[1], pool_b);
@@ -196,11 +204,17 @@ __global__ __launch_bounds__(kWdThreads, 1) void quant_attention_wide_kernel(QAt
   const uint32_t ld = (uint32_t)a.p.ld;
 
   auto aux = [](char* ring, int t) { return ring + (t & (kWdAux - 1)) * kAuxB; };
-  auto issue_slots = [&](int t) { dma4_asm(sres, (uint32_t)(t * kTileK + lane) * 4u, aux(slot_ring, t)); };
-  // the scales of tile t's keys; 0, an empty block's, where there is no key or no such slot
+  // tiles are counted from the first one
+  auto issue_slots = [&](int t) { dma4_asm(sres, (uint32_t)(key0 + t * kTileK + lane) * 4u, aux(slot_ring, t)); };
+  // whether key i of tile t is there, and its slot
+  auto has_key = [&](int t, int i, int& slot) {
+    slot = *reinterpret_cast<const int*>(aux(slot_ring, t) + i * 4);
+    return t * kTileK + i < n_keys && (uint32_t)slot < n_slots;
+  };
+  // the scales of tile t's keys
   auto issue_scales = [&](int t, rsrc_words res, char* ring) {
-    const int slot = *reinterpret_cast<const int*>(aux(slot_ring, t) + lane * 4);
-    const bool ok = t * kTileK + lane < key_end && slot >= 0 && slot < a.p.n_slots;
+    int slot;
+    const bool ok = has_key(t, lane, slot);
     dma4_asm(res, ok ? (uint32_t)((slot >> a.p.shift) * a.p.heads + g) * 4u : kAbsent, aux(ring, t));
   };
   auto issue_aux = [&](int t_slots) {
@@ -208,29 +222,40 @@ __global__ __launch_bounds__(kWdThreads, 1) void quant_attention_wide_kernel(QAt
     if (wave == 1) issue_scales(t_slots - 1, ksres, ks_ring);
     if (wave == 2) issue_scales(t_slots - 1, vsres, vs_ring);
   };
-  // This wave's rows of a tile, one 16-byte chunk of codes a lane: row kk.  Of
-  // an empty block the copies give zeros.
+  // This wave's rows of a tile, one 16-byte chunk of codes a lane: row kk.
   const int kk = wave * 8 + (lane >> 3), ch = lane & 7;
-  auto issue_codes = [&](int t, rsrc_words res, char* ring, char* scales) {
-    const int slot = *reinterpret_cast<const int*>(aux(slot_ring, t) + kk * 4);
-    const float sc = *reinterpret_cast<const float*>(aux(scales, t) + kk * 4);
+  auto issue_codes = [&](int t, rsrc_words res, char* ring) {
+    int slot;
+    const bool ok = has_key(t, kk, slot);
     const uint32_t off = (uint32_t)slot * ld + (uint32_t)g * kDh + ch * 16;
-    dma16_asm(res, sc > 0.f ? off : kAbsent, ring + (t & (kWdStages - 1)) * kCodeTileB + wave * 1024);
+    dma16_asm(res, ok ? off : kAbsent, ring + (t & (kWdStages - 1)) * kCodeTileB + wave * 1024);
   };
   // Converted rows have 16-byte chunk c of row r at c ^ (r & 15) (K) and at
   // c ^ 2 (r & 3) (V), as their fragment reads need it.
-  auto convert = [&](int t, const char* ring, char* scales, char* tile, int swizzle) {
-    const float sc = *reinterpret_cast<const float*>(aux(scales, t) + kk * 4);
-    const u32x4 w =
-        *reinterpret_cast<const u32x4*>(ring + (t & (kWdStages - 1)) * kCodeTileB + wave * 1024 + lane * 16);
+  struct Row {
+    u32x4 codes;
+    float scale;
+  };
+  auto read_row = [&](int t, const char* ring, char* scales) {
+    return Row{*reinterpret_cast<const u32x4*>(ring + (t & (kWdStages - 1)) * kCodeTileB + wave * 1024 + lane * 16),
+               *reinterpret_cast<const float*>(aux(scales, t) + kk * 4)};
+  };
+  auto convert = [&](int t, Row r, char* tile, int swizzle) {
+    // an empty block's codes stand for zeros
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(r.scale > 0.f)) != 0, 0)) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) r.codes[j] = r.scale > 0.f ? r.codes[j] : 0u;
+    }
     u32x4 c[2];
-    convert16(w, sc, c);
+    convert16(r.codes, r.scale, c);
     char* row = tile + (t & 1) * kTileB + kk * kRowB;
     *reinterpret_cast<u32x4*>(row + (((2 * ch) ^ swizzle) << 4)) = c[0];
     *reinterpret_cast<u32x4*>(row + (((2 * ch + 1) ^ swizzle) << 4)) = c[1];
   };
-  auto convert_k = [&](int t) { convert(t, k_codes, ks_ring, k_tile, kk & 15); };
-  auto convert_v = [&](int t) { convert(t, v_codes, vs_ring, v_tile, (kk & 3) << 1); };
+  auto read_k = [&](int t) { return read_row(t, k_codes, ks_ring); };
+  auto read_v = [&](int t) { return read_row(t, v_codes, vs_ring); };
+  auto convert_k = [&](int t, const Row& r) { convert(t, r, k_tile, kk & 15); };
+  auto convert_v = [&](int t, const Row& r) { convert(t, r, v_tile, (kk & 3) << 1); };
 
   const float scale = kLog2e * rsqrtf((float)kDh);
   const int krow = key_perm(lane & 31);
@@ -274,7 +299,7 @@ __global__ __launch_bounds__(kWdThreads, 1) void quant_attention_wide_kernel(QAt
   // the scaled maximum of a tile's logits, those of keys past the end made
   // -inf.  Register r of key block kb holds key 32 kb + 16 (r / 8) + 8 hl + r % 8.
   auto tile_max = [&](int t, f32x16 (&st)[2]) {
-    const int n = key_end - t * kTileK;  // > 0
+    const int n = n_keys - t * kTileK;  // > 0
     if (n < kTileK) {
       const uint64_t drop = ~0ull << n;
       const uint32_t dw[2] = {(uint32_t)drop >> (8 * hl), (uint32_t)(drop >> 32) >> (8 * hl)};
@@ -292,28 +317,27 @@ __global__ __launch_bounds__(kWdThreads, 1) void quant_attention_wide_kernel(QAt
     return fmaxf(mx, __shfl_xor(mx, 32)) * scale;
   };
 
-  if (t_lo < t_hi) {
+  if (n_t > 0) {
     // prologue: the slots of six tiles, the scales of five, the codes of four
     // K tiles and three V tiles
     if (wave == 0)
-      for (int i = 0; i < 6; ++i) issue_slots(t_lo + i);
+      for (int i = 0; i < 6; ++i) issue_slots(i);
     wait_vm_asm<0>();
     bare_barrier();
     if (wave == 1)
-      for (int i = 0; i < 5; ++i) issue_scales(t_lo + i, ksres, ks_ring);
+      for (int i = 0; i < 5; ++i) issue_scales(i, ksres, ks_ring);
     if (wave == 2)
-      for (int i = 0; i < 5; ++i) issue_scales(t_lo + i, vsres, vs_ring);
-    wait_vm_asm<0>();
-    bare_barrier();
-    issue_codes(t_lo, kres, k_codes, ks_ring);
+      for (int i = 0; i < 5; ++i) issue_scales(i, vsres, vs_ring);
+    issue_codes(0, kres, k_codes);
     for (int i = 0; i < 3; ++i) {
-      issue_codes(t_lo + i + 1, kres, k_codes, ks_ring);
-      issue_codes(t_lo + i, vres, v_codes, vs_ring);
+      issue_codes(i + 1, kres, k_codes);
+      issue_codes(i, vres, v_codes);
     }
-    wait_vm_asm<4>();  // K of two tiles, V of one
-    convert_k(t_lo);
-    convert_k(t_lo + 1);
-    convert_v(t_lo);
+    wait_vm_asm<4>();  // the scales; K of two tiles, V of one
+    bare_barrier();
+    convert_k(0, read_k(0));
+    convert_k(1, read_k(1));
+    convert_v(0, read_v(0));
     wait_lgkmcnt<0>();
     bare_barrier();
     if (live) {
@@ -322,9 +346,9 @@ __global__ __launch_bounds__(kWdThreads, 1) void quant_attention_wide_kernel(QAt
 #pragma unroll
         for (int r = 0; r < 16; ++r) st_a[kb][r] = 0.f;
 #pragma unroll
-        for (int s = 0; s < 8; ++s) st_a[kb] = mfma32x32x16(kfrag(t_lo, 8 * kb + s), qf[s], st_a[kb]);
+        for (int s = 0; s < 8; ++s) st_a[kb] = mfma32x32x16(kfrag(0, 8 * kb + s), qf[s], st_a[kb]);
       }
-      rescale(tile_max(t_lo, st_a));
+      rescale(tile_max(0, st_a));
     }
   }
   auto step = [&](int t, f32x16 (&cur)[2], f32x16 (&nxt)[2]) {
@@ -336,10 +360,10 @@ __global__ __launch_bounds__(kWdThreads, 1) void quant_attention_wide_kernel(QAt
     bare_barrier();
     issue_aux(t + 6);
     if (!live) {
-      issue_codes(t + 4, kres, k_codes, ks_ring);
-      issue_codes(t + 3, vres, v_codes, vs_ring);
-      convert_k(t + 2);
-      convert_v(t + 1);
+      issue_codes(t + 4, kres, k_codes);
+      issue_codes(t + 3, vres, v_codes);
+      convert_k(t + 2, read_k(t + 2));
+      convert_v(t + 1, read_v(t + 1));
       return;
     }
     const float m_use = m_run == -INFINITY ? 0.f : m_run;
@@ -357,8 +381,8 @@ __global__ __launch_bounds__(kWdThreads, 1) void quant_attention_wide_kernel(QAt
     // The empty asm statements keep the running sum and maximum in their place.
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      if (i == 1) issue_codes(t + 4, kres, k_codes, ks_ring);
-      if (i == 3) issue_codes(t + 3, vres, v_codes, vs_ring);
+      if (i == 1) issue_codes(t + 4, kres, k_codes);
+      if (i == 3) issue_codes(t + 3, vres, v_codes);
       if (i + kWdKAhead < 16) kf[(i + kWdKAhead) % (kWdKAhead + 1)] = kfrag(t + 1, i + kWdKAhead);
       if (i >= 16 - kWdVAhead) vf[i - (16 - kWdVAhead)] = vfrag(t, i - (16 - kWdVAhead));
       nxt[i >> 3] = mfma32x32x16(kf[i % (kWdKAhead + 1)], qf[i & 7], nxt[i >> 3]);
@@ -373,33 +397,298 @@ __global__ __launch_bounds__(kWdThreads, 1) void quant_attention_wide_kernel(QAt
       __builtin_amdgcn_sched_barrier(0);
     }
     l_part += psum;
+    Row row_k, row_v;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       if (i + kWdVAhead < 16) vf[(i + kWdVAhead) % (kWdVAhead + 1)] = vfrag(t, i + kWdVAhead);
       o_acc[i & 3] = mfma32x32x16(vf[i % (kWdVAhead + 1)], pb[i >> 3][(i >> 2) & 1], o_acc[i & 3]);
       mx = fmaxf(mx, fmaxf(nxt[i >> 3][2 * (i & 7)], nxt[i >> 3][2 * (i & 7) + 1]));
       asm volatile("" ::"v"(mx));
-      if (i == 2) convert_k(t + 2);
-      if (i == 7) convert_v(t + 1);
+      if (i == 0) row_k = read_k(t + 2);
+      if (i == 2) row_v = read_v(t + 1);
+      if (i == 5) convert_k(t + 2, row_k);
+      if (i == 9) convert_v(t + 1, row_v);
       __builtin_amdgcn_sched_barrier(0);
     }
-    if (t + 1 < t_hi) {
-      if ((t + 2) * kTileK > key_end) mx = tile_max(t + 1, nxt);
+    if (t + 1 < n_t) {
+      if ((t + 2) * kTileK > n_keys) mx = tile_max(t + 1, nxt);
       else mx = fmaxf(mx, __shfl_xor(mx, 32)) * scale;
       rescale(mx);
     }
   };
-  int t = t_lo;
-  for (; t + 1 < t_hi; t += 2) {
+  for (int t = 0; t < n_t; t += 2) {
     step(t, st_a, st_b);
-    step(t + 1, st_b, st_a);
+    if (t + 1 < n_t) step(t + 1, st_b, st_a);
   }
-  if (t < t_hi) step(t, st_a, st_b);
   wait_vm_asm<0>();  // every copy has landed before the workgroup's LDS is given away
 
   if (!live) return;
   const float l_tot = l_part + __shfl_xor(l_part, 32);
   if (q_ok) write_query(a, pair, un.split, hl, o_acc, m_run, l_tot);
+}
+
+// ============================================================================
+// quant_attention_narrow_kernel: 32 queries of one KV head and request, the
+// keys dealt to the four waves of a workgroup, which never wait for each other
+// until their results are combined: for calls with few queries, whose time is
+// reading the cache.
+// A wave reads 32-key tiles of codes two tiles ahead into registers (a lane
+// 16 bytes, eight lanes a row, which is what the address path is fast for),
+// and passes them through LDS of its own to the operands' layouts, still as
+// codes.  They are converted in registers: K by rows, times its scale, lane
+// half hl supplying dimensions 64 hl + 8 s .. + 7 to product s and the query
+// held in the same order; V by a transposing read of bytes (in each 16-lane
+// group lane i points at key i / 2, dimensions 8 (i % 2) .. + 7 and receives
+// dimension i of the 8 keys), unscaled, the scale being a factor of the weight
+// instead.  16-byte chunk c of row r lies at c ^ k_swizzle(r) (K) and
+// c ^ (r & 7) (V).  Slots are read and offsets and scales made for 64 keys at a
+// time, one key a lane.
+// ============================================================================
+constexpr int kNwWaves = 4;
+constexpr int kNwTileK = 32;
+constexpr int kNwTileB = kNwTileK * kDh;   // 4 KB of codes
+constexpr int kNwCopies = kNwTileB / 1024;
+constexpr int kNwWaveB = 2 * kNwTileB + 4 * kAuxB;  // a wave's LDS
+static_assert(kNwWaves * kNwWaveB >= 2 * 66 * 64 * 4, "room for two waves' results");
+
+__device__ __forceinline__ int k_swizzle(int r) { return (r & 3) | ((r >> 1) & 4); }
+__device__ __forceinline__ bf16x8 v_fragment(const char* lds) {
+  typedef int v2i32 __attribute__((__vector_size__(2 * sizeof(int))));
+  const v2i32 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) v2i32*)lds);
+  u32x4 c;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    c[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], 1.f, false));
+    c[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], 1.f, true));
+  }
+  return __builtin_bit_cast(bf16x8, c);
+}
+
+__global__ __launch_bounds__(64 * kNwWaves, 2) void quant_attention_narrow_kernel(QAttnArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[kNwWaves * kNwWaveB];
+
+  const Unit un = unit_of(a.rg, a.splits, 1);
+  const int g = un.g, b = un.b;
+  const int tid = threadIdx.x, lane = tid & 63, hl = lane >> 5, row = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int nr = a.rg.cu_rows[b + 1] - a.rg.cu_rows[b];
+  const int v = a.v_lo[b] + un.tile * 32 + row;
+  const bool q_ok = v < a.v_hi[b];
+  const int64_t pair = (int64_t)(a.rg.cu_rows[b] + (q_ok ? v % nr : 0)) * a.H + g * a.rep + (q_ok ? v / nr : 0);
+  const int S = a.rg.cu_keys[b + 1] - a.rg.cu_keys[b];
+  const int n_kt = (S + kNwTileK - 1) / kNwTileK;
+  const int parts = a.splits * kNwWaves, part = un.split * kNwWaves + wave;
+  const int t_lo = (int)((int64_t)part * n_kt / parts), t_hi = (int)((int64_t)(part + 1) * n_kt / parts);
+  const int key0 = t_lo * kNwTileK, n_keys = min(S, t_hi * kNwTileK) - key0;  // this wave's keys
+  const int n_t = t_hi - t_lo;
+
+  bf16x8 qf[8];
+#pragma unroll
+  for (int s = 0; s < 8; ++s) {
+    u32x4 w = {0u, 0u, 0u, 0u};
+    if (q_ok) w = *reinterpret_cast<const u32x4*>(a.q + pair * kDh + 64 * hl + 8 * s);
+    qf[s] = __builtin_bit_cast(bf16x8, w);
+  }
+
+  const uint32_t n_slots = (uint32_t)a.p.n_slots;
+  const uint32_t pool_b = (uint32_t)(a.p.n_slots * a.p.ld);  // < 2^31
+  const uint32_t scale_b = (uint32_t)(((a.p.n_slots + (1 << a.p.shift) - 1) >> a.p.shift) * a.p.heads * 4);
+  const auto kres = buffer_rsrc(a.p.codes[0], pool_b), vres = buffer_rsrc(a.p.codes[1], pool_b);
+  const auto ksres = buffer_rsrc(a.p.scales[0], scale_b), vsres = buffer_rsrc(a.p.scales[1], scale_b);
+  const auto sres = buffer_rsrc(a.slots + a.rg.cu_keys[b], (uint32_t)S * 4u);
+
+  // Tiles and 64-key groups are counted from this wave's first key.  In LDS: a
+  // tile of K and of V codes, byte offsets of two groups, scales of one.
+  char* const kt = lds + wave * kNwWaveB;
+  char* const vt = kt + kNwTileB;
+  char* const offsets = vt + kNwTileB;
+  char* const k_scales = offsets + 2 * kAuxB;
+  char* const v_scales = k_scales + kAuxB;
+  struct Scales {
+    uint32_t k, v;
+  };
+  auto load_slot = [&](int u) {
+    return (int)__builtin_amdgcn_raw_buffer_load_b32(sres, (uint32_t)(key0 + u * 64 + lane) * 4u, 0, 0);
+  };
+  auto has_key = [&](int u, int slot) { return u * 64 + lane < n_keys && (uint32_t)slot < n_slots; };
+  auto put_offset = [&](int u, int slot) {
+    const uint32_t off = (uint32_t)slot * (uint32_t)a.p.ld + (uint32_t)g * kDh;
+    *reinterpret_cast<uint32_t*>(offsets + (u & 1) * kAuxB + lane * 4) = has_key(u, slot) ? off : kAbsent;
+  };
+  auto load_scales = [&](int u, int slot, Scales& x) {
+    const uint32_t off = has_key(u, slot) ? (uint32_t)((slot >> a.p.shift) * a.p.heads + g) * 4u : kAbsent;
+    x.k = __builtin_amdgcn_raw_buffer_load_b32(ksres, off, 0, 0);
+    x.v = __builtin_amdgcn_raw_buffer_load_b32(vsres, off, 0, 0);
+  };
+  auto put_scales = [&](const Scales& x) {
+    *reinterpret_cast<uint32_t*>(k_scales + lane * 4) = x.k;
+    *reinterpret_cast<uint32_t*>(v_scales + lane * 4) = x.v;
+    return __builtin_amdgcn_ballot_w64(!(__uint_as_float(x.k) > 0.f) || !(__uint_as_float(x.v) > 0.f)) != 0;
+  };
+  const int lrow = lane >> 3, lch = lane & 7;
+  struct Codes {
+    u32x4 k[kNwCopies], v[kNwCopies];
+  };
+  auto load_codes = [&](int t, Codes& x) {
+#pragma unroll
+    for (int i = 0; i < kNwCopies; ++i) {
+      const uint32_t off =
+          *reinterpret_cast<const uint32_t*>(offsets + ((t >> 1) & 1) * kAuxB + ((t & 1) * kNwTileK + 8 * i + lrow) * 4) +
+          lch * 16;
+      x.k[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kres, off, 0, 0));
+      x.v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vres, off, 0, 0));
+    }
+  };
+  auto put_codes = [&](int t, Codes& x, bool empty) {
+    if (empty) {  // an empty block's codes stand for zeros
+#pragma unroll
+      for (int i = 0; i < kNwCopies; ++i) {
+        const int at = ((t & 1) * kNwTileK + 8 * i + lrow) * 4;
+        const bool ke = *reinterpret_cast<const float*>(k_scales + at) > 0.f;
+        const bool ve = *reinterpret_cast<const float*>(v_scales + at) > 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x.k[i][j] = ke ? x.k[i][j] : 0u;
+          x.v[i][j] = ve ? x.v[i][j] : 0u;
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kNwCopies; ++i) {
+      const int r = 8 * i + lrow;
+      *reinterpret_cast<u32x4*>(kt + r * kDh + ((lch ^ k_swizzle(r)) << 4)) = x.k[i];
+      *reinterpret_cast<u32x4*>(vt + r * kDh + ((lch ^ (r & 7)) << 4)) = x.v[i];
+    }
+  };
+
+  const float scale = kLog2e * rsqrtf((float)kDh);
+  const int krow = key_perm(row), k_sw = k_swizzle(krow);
+  const int vgrp = lane >> 4, gi = lane & 15;
+  const int v_key = 8 * (vgrp >> 1) + (gi >> 1);
+  const int v_off = v_key * kDh + (gi & 1) * 8, v_sw = v_key & 7, v_ch = vgrp & 1;
+
+  f32x16 o_acc[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o_acc[d][r] = 0.f;
+  float m_run = -INFINITY, l_part = 0.f;
+
+  auto step = [&](int t) {
+    const float ks = *reinterpret_cast<const float*>(k_scales + ((t & 1) * kNwTileK + krow) * 4);
+    f32x16 st;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) st[r] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const u32x4 w = *reinterpret_cast<const u32x4*>(kt + krow * kDh + (((4 * hl + i) ^ k_sw) << 4));
+      u32x4 c[2];
+      convert16(w, ks, c);
+      st = mfma32x32x16(__builtin_bit_cast(bf16x8, c[0]), qf[2 * i], st);
+      st = mfma32x32x16(__builtin_bit_cast(bf16x8, c[1]), qf[2 * i + 1], st);
+    }
+    // register r holds key 16 (r / 8) + 8 hl + r % 8
+    const int n = n_keys - t * kNwTileK;  // > 0
+    if (n < kNwTileK) {
+      const uint32_t drop = (~0u << n) >> (8 * hl);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st[r] = (drop >> (16 * (r >> 3) + (r & 7))) & 1u ? -INFINITY : st[r];
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[r]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32)) * scale;
+    const bool bump = mx > m_run + 8.f;
+    if (__builtin_amdgcn_ballot_w64(bump)) {
+      const float alpha = bump ? __builtin_amdgcn_exp2f(m_run - mx) : 1.f;
+      m_run = bump ? mx : m_run;
+      l_part *= alpha;
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o_acc[d][r] *= alpha;
+    }
+    const float m_use = m_run == -INFINITY ? 0.f : m_run;
+    const char* vs = v_scales + ((t & 1) * kNwTileK + 8 * hl) * 4;
+    bf16x8 pb[2];
+#pragma unroll
+    for (int g2 = 0; g2 < 2; ++g2) {
+      f32x4 sv[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) sv[j] = *reinterpret_cast<const f32x4*>(vs + (16 * g2 + 4 * j) * 4);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(st[8 * g2 + j], scale, -m_use));
+        l_part += e;
+        pb[g2][j] = (bf16)(e * sv[j >> 2][j & 3]);
+      }
+    }
+#pragma unroll
+    for (int g2 = 0; g2 < 2; ++g2)
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+        o_acc[d] = mfma32x32x16(v_fragment(vt + 16 * g2 * kDh + v_off + (((2 * d + v_ch) ^ v_sw) << 4)), pb[g2],
+                                o_acc[d]);
+  };
+
+  if (n_t > 0) {
+    Codes x0, x1;
+    Scales sa, sb;
+    const int s0 = load_slot(0), s1 = load_slot(1);
+    int next = load_slot(2);
+    put_offset(0, s0);
+    load_codes(0, x0);
+    load_codes(1, x1);
+    load_scales(0, s0, sa);
+    put_offset(1, s1);
+    load_scales(1, s1, sb);
+    for (int t = 0; t < n_t; t += 2) {
+      const int u = t >> 1;
+      const bool empty = put_scales(sa);
+      put_codes(t, x0, empty);
+      load_codes(t + 2, x0);
+      step(t);
+      put_codes(t + 1, x1, empty);
+      load_codes(t + 3, x1);
+      put_offset(u + 2, next);  // over group u's
+      sa = sb;
+      load_scales(u + 2, next, sb);
+      next = load_slot(u + 3);
+      if (t + 1 < n_t) step(t + 1);
+    }
+  }
+
+  // the waves' results, lane by lane: 1 into 0 and 3 into 2, then 2 into 0
+  float l = l_part + __shfl_xor(l_part, 32), m = m_run;
+  float* const res = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int round = 0; round < 2; ++round) {
+    const bool give = round == 0 ? (wave & 1) : wave == 2, take = round == 0 ? !(wave & 1) : wave == 0;
+    float* const at = res + (round == 0 ? wave >> 1 : 0) * (66 * 64);
+    __syncthreads();
+    if (give) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) at[(16 * d + r) * 64 + lane] = o_acc[d][r];
+      at[64 * 64 + lane] = m;
+      at[65 * 64 + lane] = l;
+    }
+    __syncthreads();
+    if (take) {
+      const float m2 = at[64 * 64 + lane], l2 = at[65 * 64 + lane];
+      const float mn = fmaxf(m, m2);
+      const float f0 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+      const float f1 = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m2 - mn);
+      l = l * f0 + l2 * f1;
+      m = mn;
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o_acc[d][r] = o_acc[d][r] * f0 + at[(16 * d + r) * 64 + lane] * f1;
+    }
+  }
+  if (wave == 0 && q_ok) write_query(a, pair, un.split, hl, o_acc, m, l);
 }
 
 // Combines the key splits of each (row, head): m = max_s m_s, O = sum_s
@@ -462,6 +751,41 @@ size_t quant_attention_part_bytes(int64_t pairs) {
   return (size_t)std::min<int64_t>(kPartPairs, pairs * kMaxSplits) * (kDh + 2) * sizeof(float);
 }
 
+namespace {
+
+// Estimated time (us) of `units` (query tile, KV head) pairs over n_kt 64-key
+// tiles and the key splits that give it, within `fit`.  Measured: a launch and
+// its first loads 6; a step of the narrow kernel (32 keys a wave) 0.95, or 1.65
+// with two workgroups on a CU; a tile of the wide kernel 1.9, one workgroup a
+// CU; a merge 3.5 and its partials at 3 TB/s.
+struct Cost {
+  double us;
+  int splits;
+};
+Cost narrow_cost(int64_t units, int n_kt, int64_t pairs, int64_t fit) {
+  Cost best = {1e30, 1};
+  for (int s = 1; s <= std::min<int64_t>(fit, kMaxSplits); ++s) {
+    const int64_t wgs = units * s, rounds = wgs / 512, rest = wgs % 512;
+    const int steps = (2 * n_kt + kNwWaves * s - 1) / (kNwWaves * s);
+    const double us = 6.0 + steps * (1.65 * rounds + (rest == 0 ? 0.0 : rest <= 256 ? 0.95 : 1.65)) +
+                      (s > 1 ? 3.5 + 2.0 * s * pairs * (kDh + 2) * 4 / 3e6 : 0.0);
+    if (us < best.us) best = {us, s};
+    if (steps == 1) break;
+  }
+  return best;
+}
+Cost wide_cost(int64_t units, int n_kt, int64_t pairs, int64_t fit) {
+  Cost best = {1e30, 1};
+  for (int s = 1; s <= std::min<int64_t>(std::min<int64_t>(fit, kMaxSplits), std::max(n_kt, 1)); ++s) {
+    const double us = 6.0 + 1.9 * ((n_kt + s - 1) / s) * (double)((units * s + 255) / 256) +
+                      (s > 1 ? 3.5 + 2.0 * s * pairs * (kDh + 2) * 4 / 3e6 : 0.0);
+    if (us < best.us) best = {us, s};
+  }
+  return best;
+}
+
+}  // namespace
+
 hipError_t launch_quant_attention(const Ragged& rg, int H, const QuantPool& p, const void* q, const int32_t* read_slots,
                                   void* out, float* lse, float* part, size_t part_bytes, hipStream_t s) {
   const int64_t rows = rg.cu_rows[rg.batch];
@@ -476,20 +800,51 @@ hipError_t launch_quant_attention(const Ragged& rg, int H, const QuantPool& p, c
   a.rep = H / p.heads;
   a.rg = rg;
   const int64_t pairs = rows * H;
-  int64_t tiles = 0;
-  int max_kt = 0;
+  // query tiles of each kernel, and of the wide kernel on whole tiles with the
+  // narrow one behind it on what is left of each request
+  int64_t narrow = 0, wide = 0, whole = 0, rest = 0;
+  int n_kt = 0;
   for (int b = 0; b < rg.batch; ++b) {
-    a.rg.tile_start[b] = (int)tiles;
-    tiles += ((int64_t)(rg.cu_rows[b + 1] - rg.cu_rows[b]) * a.rep + 255) / 256;
-    max_kt = std::max(max_kt, (rg.cu_keys[b + 1] - rg.cu_keys[b] + kTileK - 1) / kTileK);
+    const int64_t n = (int64_t)(rg.cu_rows[b + 1] - rg.cu_rows[b]) * a.rep;
+    narrow += (n + 31) / 32;
+    wide += (n + kWdTileQ - 1) / kWdTileQ;
+    whole += n / kWdTileQ;
+    rest += (n % kWdTileQ + 31) / 32;
+    n_kt = std::max(n_kt, (rg.cu_keys[b + 1] - rg.cu_keys[b] + kTileK - 1) / kTileK);
   }
-  a.rg.tile_start[rg.batch] = (int)tiles;
-  const int64_t fit = (int64_t)(part_bytes / ((kDh + 2) * sizeof(float))) / pairs;
-  int splits = (int)std::max<int64_t>(1, std::min<int64_t>({fit, kMaxSplits, (int64_t)max_kt, (512 + tiles * p.heads - 1) / (tiles * p.heads)}));
-  a.splits = splits;
-  a.part_o = part;
-  a.part_ml = part ? part + (size_t)splits * pairs * kDh : nullptr;
-  hipLaunchKernelGGL(quant_attention_wide_kernel, dim3((unsigned)(tiles * p.heads * splits)), dim3(512), 0, s, a);
+  const int64_t fit = std::max<int64_t>(1, (int64_t)(part_bytes / ((kDh + 2) * sizeof(float))) / pairs);
+  const Cost cn = narrow_cost(narrow * p.heads, n_kt, pairs, fit), cw = wide_cost(wide * p.heads, n_kt, pairs, fit);
+  // the two launches write no partials: a merge would cover every row
+  const double both = whole && rest ? wide_cost(whole * p.heads, n_kt, pairs, 1).us +
+                                          narrow_cost(rest * p.heads, n_kt, pairs, 1).us
+                                    : 1e30;
+  // one launch over each request's queries from `from` whole tiles on
+  auto launch = [&](bool is_wide, bool skip_whole, bool only_whole, int splits) {
+    const int tq = is_wide ? kWdTileQ : 32;
+    int tiles = 0;
+    for (int b = 0; b < rg.batch; ++b) {
+      const int n = (rg.cu_rows[b + 1] - rg.cu_rows[b]) * a.rep, w = n - n % kWdTileQ;
+      a.rg.tile_start[b] = tiles;
+      a.v_lo[b] = skip_whole ? w : 0;
+      a.v_hi[b] = only_whole ? w : n;
+      tiles += (a.v_hi[b] - a.v_lo[b] + tq - 1) / tq;
+    }
+    a.rg.tile_start[rg.batch] = tiles;
+    a.splits = splits;
+    a.part_o = part;
+    a.part_ml = part ? part + (size_t)splits * pairs * kDh : nullptr;
+    const dim3 grid((unsigned)((int64_t)tiles * p.heads * splits));
+    if (is_wide) hipLaunchKernelGGL(quant_attention_wide_kernel, grid, dim3(kWdThreads), 0, s, a);
+    else hipLaunchKernelGGL(quant_attention_narrow_kernel, grid, dim3(64 * kNwWaves), 0, s, a);
+  };
+  if (both < std::min(cn.us, cw.us)) {
+    launch(true, false, true, 1);
+    launch(false, true, false, 1);
+    return hipGetLastError();
+  }
+  const bool is_wide = cw.us < cn.us;
+  const int splits = is_wide ? cw.splits : cn.splits;
+  launch(is_wide, false, false, splits);
   if (splits > 1)
     hipLaunchKernelGGL(quant_attention_merge_kernel, dim3((unsigned)((pairs + 7) / 8)), dim3(256), 0, s,
                        (const float*)a.part_o, (const float*)a.part_ml, splits, pairs, a.out, lse);
