@@ -231,7 +231,9 @@ __global__ __launch_bounds__(kWdThreads, 1) void quant_attention_wide_kernel(QAt
     dma16_asm(res, ok ? off : kAbsent, ring + (t & (kWdStages - 1)) * kCodeTileB + wave * 1024);
   };
   // Converted rows have 16-byte chunk c of row r at c ^ (r & 15) (K) and at
-  // c ^ 2 (r & 3) (V), as their fragment reads need it.
+  // c ^ (4 (r & 3) ^ (r & 1)) (V): sixteen lanes' fragment reads and writes of
+  // K, and 32 lanes' transposing reads of V (four rows of four chunks), then
+  // cover all the banks.
   struct Row {
     u32x4 codes;
     float scale;
@@ -255,7 +257,7 @@ __global__ __launch_bounds__(kWdThreads, 1) void quant_attention_wide_kernel(QAt
   auto read_k = [&](int t) { return read_row(t, k_codes, ks_ring); };
   auto read_v = [&](int t) { return read_row(t, v_codes, vs_ring); };
   auto convert_k = [&](int t, const Row& r) { convert(t, r, k_tile, kk & 15); };
-  auto convert_v = [&](int t, const Row& r) { convert(t, r, v_tile, (kk & 3) << 1); };
+  auto convert_v = [&](int t, const Row& r) { convert(t, r, v_tile, ((kk & 3) << 2) ^ (kk & 1)); };
 
   const float scale = kLog2e * rsqrtf((float)kDh);
   const int krow = key_perm(lane & 31);
@@ -263,7 +265,7 @@ __global__ __launch_bounds__(kWdThreads, 1) void quant_attention_wide_kernel(QAt
   const int vgrp = lane >> 4, gi = lane & 15;
   const int v_key = 8 * (vgrp >> 1) + (gi >> 2);
   const int v_chunk = 2 * (vgrp & 1) + ((gi & 3) >> 1);
-  const int v_byte = (gi & 1) * 8, v_sw = (gi >> 2) << 1;
+  const int v_byte = (gi & 1) * 8, v_sw = (gi & 12) ^ ((gi >> 2) & 1);
   auto kfrag = [&](int t, int i) {
     const int kb = i >> 3, s = i & 7;
     return *reinterpret_cast<const bf16x8*>(k_tile + (t & 1) * kTileB + kb * 32 * kRowB + k_off +
@@ -800,33 +802,45 @@ hipError_t launch_quant_attention(const Ragged& rg, int H, const QuantPool& p, c
   a.rep = H / p.heads;
   a.rg = rg;
   const int64_t pairs = rows * H;
-  // query tiles of each kernel, and of the wide kernel on whole tiles with the
-  // narrow one behind it on what is left of each request
-  int64_t narrow = 0, wide = 0, whole = 0, rest = 0;
+  // query tiles of each kernel, and of the wide kernel with the narrow one
+  // behind it on what is left of a request behind its whole tiles, where that
+  // is at most kRest[i] queries
+  constexpr int kRest[3] = {64, 128, kWdTileQ - 1};
+  int64_t narrow = 0, wide = 0, both_wide[3] = {}, both_narrow[3] = {};
   int n_kt = 0;
   for (int b = 0; b < rg.batch; ++b) {
     const int64_t n = (int64_t)(rg.cu_rows[b + 1] - rg.cu_rows[b]) * a.rep;
     narrow += (n + 31) / 32;
     wide += (n + kWdTileQ - 1) / kWdTileQ;
-    whole += n / kWdTileQ;
-    rest += (n % kWdTileQ + 31) / 32;
+    for (int i = 0; i < 3; ++i) {
+      const bool few = n % kWdTileQ <= kRest[i];
+      both_wide[i] += few ? n / kWdTileQ : (n + kWdTileQ - 1) / kWdTileQ;
+      both_narrow[i] += few ? (n % kWdTileQ + 31) / 32 : 0;
+    }
     n_kt = std::max(n_kt, (rg.cu_keys[b + 1] - rg.cu_keys[b] + kTileK - 1) / kTileK);
   }
   const int64_t fit = std::max<int64_t>(1, (int64_t)(part_bytes / ((kDh + 2) * sizeof(float))) / pairs);
   const Cost cn = narrow_cost(narrow * p.heads, n_kt, pairs, fit), cw = wide_cost(wide * p.heads, n_kt, pairs, fit);
   // the two launches write no partials: a merge would cover every row
-  const double both = whole && rest ? wide_cost(whole * p.heads, n_kt, pairs, 1).us +
-                                          narrow_cost(rest * p.heads, n_kt, pairs, 1).us
-                                    : 1e30;
-  // one launch over each request's queries from `from` whole tiles on
-  auto launch = [&](bool is_wide, bool skip_whole, bool only_whole, int splits) {
+  double both_us = 1e30;
+  int both = 0;
+  for (int i = 0; i < 3; ++i) {
+    if (!both_wide[i] || !both_narrow[i]) continue;
+    const double us = wide_cost(both_wide[i] * p.heads, n_kt, pairs, 1).us +
+                      narrow_cost(both_narrow[i] * p.heads, n_kt, pairs, 1).us;
+    if (us < both_us) both_us = us, both = i;
+  }
+  // one launch over each request's queries: all of them, or those left to (or
+  // by) the other kernel
+  auto launch = [&](bool is_wide, bool share, int splits) {
     const int tq = is_wide ? kWdTileQ : 32;
     int tiles = 0;
     for (int b = 0; b < rg.batch; ++b) {
-      const int n = (rg.cu_rows[b + 1] - rg.cu_rows[b]) * a.rep, w = n - n % kWdTileQ;
+      const int n = (rg.cu_rows[b + 1] - rg.cu_rows[b]) * a.rep;
+      const int cut = n % kWdTileQ <= kRest[both] ? n - n % kWdTileQ : n;
       a.rg.tile_start[b] = tiles;
-      a.v_lo[b] = skip_whole ? w : 0;
-      a.v_hi[b] = only_whole ? w : n;
+      a.v_lo[b] = share && !is_wide ? cut : 0;
+      a.v_hi[b] = share && is_wide ? cut : n;
       tiles += (a.v_hi[b] - a.v_lo[b] + tq - 1) / tq;
     }
     a.rg.tile_start[rg.batch] = tiles;
@@ -837,14 +851,14 @@ hipError_t launch_quant_attention(const Ragged& rg, int H, const QuantPool& p, c
     if (is_wide) hipLaunchKernelGGL(quant_attention_wide_kernel, grid, dim3(kWdThreads), 0, s, a);
     else hipLaunchKernelGGL(quant_attention_narrow_kernel, grid, dim3(64 * kNwWaves), 0, s, a);
   };
-  if (both < std::min(cn.us, cw.us)) {
-    launch(true, false, true, 1);
-    launch(false, true, false, 1);
+  if (both_us < std::min(cn.us, cw.us)) {
+    launch(true, true, 1);
+    launch(false, true, 1);
     return hipGetLastError();
   }
   const bool is_wide = cw.us < cn.us;
   const int splits = is_wide ? cw.splits : cn.splits;
-  launch(is_wide, false, false, splits);
+  launch(is_wide, false, splits);
   if (splits > 1)
     hipLaunchKernelGGL(quant_attention_merge_kernel, dim3((unsigned)((pairs + 7) / 8)), dim3(256), 0, s,
                        (const float*)a.part_o, (const float*)a.part_ml, splits, pairs, a.out, lse);
