@@ -577,17 +577,25 @@ def _quant_check(dims: Dims, pool: QuantPool, *tensors):
     """The pool fits dims, and everything is on the current device."""
     if pool.heads != dims.n_kv_heads or pool.width < dims.n_kv_heads * dims.head_dim:
         raise ValueError("the pool's rows do not hold dims.n_kv_heads heads of dims.head_dim")
-    if pool.device.type != "cuda" or pool.device.index != torch.cuda.current_device():
-        raise ValueError(f"the pool is on {pool.device}, not on the current device")
+    device = pool.device
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError(f"the pool is on {device}, not on the current device")
     for t in tensors:
-        if t is not None and t.device != pool.device:
-            raise ValueError(f"a tensor is on {t.device} and the pool on {pool.device}")
+        if t.device != device:
+            raise ValueError(f"a tensor is on {t.device} and the pool on {device}")
 
 
-def _quant_rows(dims: Dims, t: torch.Tensor, n: int, name: str):
-    if (t.dtype != torch_dtype(dims) or t.dim() != 2 or t.shape[0] != n
-            or t.shape[1] != dims.n_kv_heads * dims.head_dim or t.stride(1) != 1):
-        raise TypeError(f"{name} must be [{n}, n_kv_heads * head_dim] of dims' type with contiguous rows")
+def _quant_rows(dims: Dims, k: torch.Tensor, v: torch.Tensor, n: int) -> int:
+    """The row stride of k and v: [n, n_kv_heads * head_dim] of dims' type."""
+    shape, dt = (n, dims.n_kv_heads * dims.head_dim), torch_dtype(dims)
+    ld = k.stride()
+    if k.dtype != dt or v.dtype != dt or k.shape != shape or v.shape != shape or ld[1] != 1:
+        raise TypeError(f"rows of K and V must be {list(shape)} tensors of dims' type with contiguous rows")
+    if n <= 1:
+        return shape[1] if v.stride(1) == 1 else 0
+    if v.stride() != ld:
+        raise ValueError("rows of K and V must have the same strides")
+    return ld[0]
 
 
 def acache_quant_store(dims: Dims, pool: QuantPool, k_src: torch.Tensor, v_src: torch.Tensor,
@@ -595,17 +603,13 @@ def acache_quant_store(dims: Dims, pool: QuantPool, k_src: torch.Tensor, v_src: 
     """Rows i of K and V become the values of slots dst_slots[i]."""
     _dev_i32(dst_slots, "dst_slots")
     n = dst_slots.numel()
-    for t, name in ((k_src, "k_src"), (v_src, "v_src")):
-        _quant_rows(dims, t, n, name)
-    if n > 1 and k_src.stride(0) != v_src.stride(0):
-        raise ValueError("k_src and v_src must have the same row stride")
+    ld = _quant_rows(dims, k_src, v_src, n)
     if ws is None:
         ws = quant_workspace(dims, 0, pool)
     _quant_check(dims, pool, k_src, v_src, dst_slots, ws)
-    ld = k_src.stride(0) if n > 1 else k_src.shape[1]
     _check("acache_quant_store", lib.acache_quant_store(
         ctypes.byref(dims), pool.ref, k_src.data_ptr(), v_src.data_ptr(), ld, n, dst_slots.data_ptr(), ws.data_ptr(),
-        ws.numel() * ws.element_size(), _stream(stream)))
+        ws.nbytes, _stream(stream)))
 
 
 def acache_quant_load(dims: Dims, pool: QuantPool, slots: torch.Tensor, k_out: Optional[torch.Tensor] = None,
@@ -615,15 +619,11 @@ def acache_quant_load(dims: Dims, pool: QuantPool, slots: torch.Tensor, k_out: O
     _dev_i32(slots, "slots")
     n = slots.numel()
     if k_out is None and v_out is None:
-        k_out, v_out = (torch.empty((n, dims.n_kv_heads * dims.head_dim), dtype=torch_dtype(dims), device=slots.device)
-                        for _ in range(2))
-    given = [t for t in (k_out, v_out) if t is not None]
-    for t in given:
-        _quant_rows(dims, t, n, "k_out and v_out")
-    if n > 1 and given[0].stride(0) != given[-1].stride(0):
-        raise ValueError("k_out and v_out must have the same row stride")
-    _quant_check(dims, pool, slots, *given)
-    ld = given[0].stride(0) if n > 1 else given[0].shape[1]
+        k_out = torch.empty((n, dims.n_kv_heads * dims.head_dim), dtype=torch_dtype(dims), device=slots.device)
+        v_out = torch.empty_like(k_out)
+    k, v = k_out if k_out is not None else v_out, v_out if v_out is not None else k_out
+    ld = _quant_rows(dims, k, v, n)
+    _quant_check(dims, pool, slots, k, v)
     _check("acache_quant_load", lib.acache_quant_load(
         ctypes.byref(dims), pool.ref, slots.data_ptr(), n, _ptr(k_out), _ptr(v_out), ld, _stream(stream)))
     return k_out, v_out
@@ -647,10 +647,10 @@ def acache_quant_attention(dims: Dims, cu_rows, cu_keys, q: torch.Tensor, read_s
     if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous()
                             or lse.numel() < rows * dims.n_heads):
         raise TypeError("lse must be a contiguous float32 tensor of [rows, n_heads] values")
-    _quant_check(dims, pool, q, read_slots, out, lse, ws)
+    _quant_check(dims, pool, *(t for t in (q, read_slots, out, lse, ws) if t is not None))
     _check("acache_quant_attention", lib.acache_quant_attention(
         ctypes.byref(dims), ctypes.byref(rg), q.data_ptr(), read_slots.data_ptr(), pool.ref, out.data_ptr(),
-        _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)))
+        _ptr(lse), _ptr(ws), 0 if ws is None else ws.nbytes, _stream(stream)))
     return out
 
 

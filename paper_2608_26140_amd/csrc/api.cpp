@@ -967,7 +967,8 @@ acache_status acache_quant_store(const acache_dims* dims, const acache_quant_poo
   const int64_t es = (int64_t)elem_size(dims->dtype);
   CHECK(src_ld >= (int64_t)p.heads * p.head_dim, ACACHE_ERR_SHAPE);
   CHECK(aligned16(k_src) && aligned16(v_src) && (src_ld * es) % 16 == 0, ACACHE_ERR_ALIGN);
-  CHECK(p.heads <= 32767, ACACHE_ERR_UNSUPPORTED);  // K and V of every head are a grid dimension
+  // a workgroup for every `block` rows, K and V of every head
+  CHECK(((int64_t)n / pool->block + 1) * 2 * p.heads < ((int64_t)1 << 31), ACACHE_ERR_UNSUPPORTED);
   CHECK(ws && ((uintptr_t)ws & 3u) == 0 && ws_bytes >= quant_map_bytes(p.n_slots, p.shift), ACACHE_ERR_WORKSPACE);
   LAUNCH_T(ACACHE_K_SCATTER, stream,
            launch_quant_store(dims->dtype, p, k_src, v_src, src_ld, n, dst_slots, (int32_t*)ws, stream));

@@ -29,36 +29,22 @@ __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
 }
 
 // ============================================================================
-// Store.  The rows of a call may name slots in any order, so a block's new
-// rows are found through a map from slots to rows in the workspace: one
-// launch marks the slots that are named (the entries of the others stay what
-// they were), the next leaves the highest row of each, and the one that
-// quantises takes an entry for a row of this call only where that row's slot
-// is the entry's own, which no stale entry can pretend.  A block is quantised
-// by the workgroups of one of its rows (its highest), one for each KV head
-// and for K and V: the maximum over the new rows, the scale, the codes, and
-// the entries that stay.
+// Store.  A block is quantised by the workgroups of one of its rows, the last
+// that names one of its slots, one workgroup for each KV head and for K and V:
+// the maximum over the new rows, the scale, the codes, and the entries that
+// stay.  The rows of a call may name slots in any order, so a block's rows are
+// found through a map from its slots to the last row of each.
+//   Up to kSmallRows rows every workgroup reads all the call's slots and makes
+// its block's map in LDS: one launch.
+//   Beyond, the map lies in the workspace: a launch marks the slots that are
+// named (the entries of the others stay what they were), the next leaves the
+// last row of each, and the one that quantises takes an entry for a row of
+// this call only where that row's slot is the entry's own, which no stale entry
+// can pretend.
+// Bound by HBM: 3 bytes an element of bf16.  Workgroups of neighbouring heads
+// are neighbours in the grid, so that whole rows are read and written together.
 // ============================================================================
-__global__ __launch_bounds__(kThreads) void quant_clear_kernel(const int32_t* __restrict__ slots, int n,
-                                                               int64_t n_slots, int shift, int32_t* __restrict__ row_of,
-                                                               int32_t* __restrict__ last_of) {
-  const int i = blockIdx.x * kThreads + threadIdx.x;
-  if (i >= n) return;
-  const int s = slots[i];
-  if (s < 0 || s >= n_slots) return;
-  row_of[s] = -1;
-  last_of[s >> shift] = -1;
-}
-__global__ __launch_bounds__(kThreads) void quant_map_kernel(const int32_t* __restrict__ slots, int n, int64_t n_slots,
-                                                             int shift, int32_t* __restrict__ row_of,
-                                                             int32_t* __restrict__ last_of) {
-  const int i = blockIdx.x * kThreads + threadIdx.x;
-  if (i >= n) return;
-  const int s = slots[i];
-  if (s < 0 || s >= n_slots) return;
-  atomicMax(row_of + s, i);
-  atomicMax(last_of + (s >> shift), i);
-}
+constexpr int kSmallRows = 1024;
 
 template <typename T>
 struct StoreArgs {
@@ -72,97 +58,154 @@ struct StoreArgs {
   int n, heads, head_dim, shift;
 };
 
-// IT: 8-element pieces of a block and head for each thread.
+// The last row of a run of rows in one block: a block's last row is one.
+__device__ __forceinline__ bool ends_run(const int32_t* slots, int i, int n, int shift) {
+  return i + 1 == n || (slots[i + 1] >> shift) != (slots[i] >> shift);
+}
+
+__global__ __launch_bounds__(kThreads) void quant_clear_kernel(const int32_t* __restrict__ slots, int n,
+                                                               int64_t n_slots, int shift, int32_t* __restrict__ row_of,
+                                                               int32_t* __restrict__ last_of) {
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i >= n) return;
+  const int s = slots[i];
+  if (s < 0 || s >= n_slots) return;
+  row_of[s] = -1;
+  if (ends_run(slots, (int)i, n, shift)) last_of[s >> shift] = -1;
+}
+// (64 rows raising one entry of last_of would queue for it: 7372 rows took 16
+// us so, the ends of runs alone RRR)
+__global__ __launch_bounds__(kThreads) void quant_map_kernel(const int32_t* __restrict__ slots, int n, int64_t n_slots,
+                                                             int shift, int32_t* __restrict__ row_of,
+                                                             int32_t* __restrict__ last_of) {
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i >= n) return;
+  const int s = slots[i];
+  if (s < 0 || s >= n_slots) return;
+  atomicMax(row_of + s, (int)i);
+  if (ends_run(slots, (int)i, n, shift)) atomicMax(last_of + (s >> shift), (int)i);
+}
+
+// Quantises one block and head from its map win (LDS): the row stored at each
+// slot, -1 where none is.  IT: 8-element pieces of the block for each thread.
 template <typename T, int IT>
-__global__ __launch_bounds__(kThreads) void quant_store_kernel(StoreArgs<T> a) {
-  __shared__ int32_t win[kMaxBlock];   // the row stored at each slot of the block, -1: none
-  __shared__ int32_t owned[kMaxBlock];
-  __shared__ int n_owned;
-  __shared__ float red[kThreads / 64];
-  __shared__ int missing;
-  const int tid = threadIdx.x, block = 1 << a.shift;
-  const int which = (int)blockIdx.y >= a.heads, g = blockIdx.y - which * a.heads;
-  if (tid == 0) n_owned = 0;
-  __syncthreads();
-  const int i0 = blockIdx.x << a.shift;
-  if (tid < block && tid < a.n - i0) {
-    const int s = a.slots[i0 + tid];
-    if (s >= 0 && s < a.n_slots && a.last_of[s >> a.shift] == i0 + tid) owned[atomicAdd(&n_owned, 1)] = s >> a.shift;
-  }
-  __syncthreads();
+__device__ __forceinline__ void store_block(const StoreArgs<T>& a, int which, int g, int blk, const int32_t* win,
+                                            float* red, int* missing) {
+  const int tid = threadIdx.x;
+  const int64_t first = (int64_t)blk << a.shift;
   const int chunks = a.head_dim >> 3, items = chunks << a.shift;
   const T* src = a.src[which] + g * a.head_dim;
   uint8_t* codes = a.codes[which] + g * a.head_dim;
-  for (int o = 0; o < n_owned; ++o) {
-    const int blk = owned[o];
-    const int64_t first = (int64_t)blk << a.shift;
+  float* sp = a.scales[which] + (int64_t)blk * a.heads + g;
+  const float old = *sp;
+  float v[IT][8];
+  float mx = 0.f;
+#pragma unroll
+  for (int it = 0; it < IT; ++it) {
+    const int item = it * kThreads + tid, r = item / chunks, c = item - r * chunks;
+    const int w = item < items ? win[r] : -1;
+    if (w >= 0) {
+      load8(src + (int64_t)w * a.src_ld + c * 8, v[it]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[it][j] = 0.f;
+    }
+  }
+  if (tid < 1 << a.shift && first + tid < a.n_slots && win[tid] < 0) *missing = 1;
+#pragma unroll
+  for (int it = 0; it < IT; ++it)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) mx = fmaxf(mx, fabsf(v[it][j]) < INFINITY ? fabsf(v[it][j]) : 0.f);
+  mx = wave_max(mx);
+  if ((tid & 63) == 0) red[tid >> 6] = mx;
+  __syncthreads();
+  mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  const int was = old > 0.f ? (int)(__float_as_uint(old) >> 23) : 0;
+  int e = scale_byte(mx);
+  if (*missing && was) e = max(e, min(was, kMaxScaleByte));
+  const float inv = pow2_byte(254 - e);
+#pragma unroll
+  for (int it = 0; it < IT; ++it) {
+    const int item = it * kThreads + tid, r = item / chunks, c = item - r * chunks;
+    if (item >= items || first + r >= a.n_slots) continue;
+    uint8_t* p = codes + (first + r) * a.ld + c * 8;
+    if (win[r] >= 0) {
+      float y[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = code_arg(v[it][j], inv);
+      *reinterpret_cast<u32x2*>(p) = u32x2{encode4(y[0], y[1], y[2], y[3]), encode4(y[4], y[5], y[6], y[7])};
+    } else if (!was) {
+      *reinterpret_cast<u32x2*>(p) = u32x2{0u, 0u};  // of an empty block: reads as zero before and after
+    } else if (e > was) {
+      const u32x2 w = *reinterpret_cast<const u32x2*>(p);
+      float lo[4], hi[4];
+      decode4(w[0], lo);
+      decode4(w[1], hi);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        lo[j] = __builtin_amdgcn_ldexpf(lo[j], was - e);
+        hi[j] = __builtin_amdgcn_ldexpf(hi[j], was - e);
+      }
+      *reinterpret_cast<u32x2*>(p) = u32x2{encode4(lo[0], lo[1], lo[2], lo[3]), encode4(hi[0], hi[1], hi[2], hi[3])};
+    }
+  }
+  if (tid == 0) *sp = pow2_byte(e);  // every thread read the old scale ahead of the barrier
+}
+
+template <typename T, int IT, bool SMALL>
+__global__ __launch_bounds__(kThreads) void quant_store_kernel(StoreArgs<T> a) {
+  __shared__ int32_t all[SMALL ? kSmallRows : 1];  // the call's slots, -1 those that are not there
+  __shared__ int32_t win[kMaxBlock];
+  __shared__ int32_t found[kMaxBlock];  // rows of this workgroup's that may be their block's last
+  __shared__ int n_found, missing;
+  __shared__ float red[kThreads / 64];
+  const int tid = threadIdx.x, block = 1 << a.shift;
+  const unsigned chunk = blockIdx.x / (2u * a.heads), h = blockIdx.x - chunk * (2u * a.heads);
+  const int which = (int)h >= a.heads, g = (int)h - which * a.heads;
+  const int i0 = (int)chunk << a.shift;
+  if (tid == 0) n_found = 0;
+  if constexpr (SMALL) {
+    for (int i = tid; i < a.n; i += kThreads) {
+      const int s = a.slots[i];
+      all[i] = s >= 0 && s < a.n_slots ? s : -1;
+    }
+  }
+  __syncthreads();
+  if (tid < block && tid < a.n - i0) {
+    if constexpr (SMALL) {
+      if (all[i0 + tid] >= 0 && ends_run(all, i0 + tid, a.n, a.shift)) found[atomicAdd(&n_found, 1)] = i0 + tid;
+    } else {
+      const int s = a.slots[i0 + tid];
+      if (s >= 0 && s < a.n_slots && a.last_of[s >> a.shift] == i0 + tid) found[atomicAdd(&n_found, 1)] = s >> a.shift;
+    }
+  }
+  __syncthreads();
+  for (int o = 0; o < n_found; ++o) {
+    int blk = found[o];
+    if constexpr (SMALL) {
+      const int row = blk;
+      blk = all[row] >> a.shift;
+      int later = 0;
+      for (int i = row + 1 + tid; i < a.n; i += kThreads) later |= all[i] >= 0 && all[i] >> a.shift == blk;
+      if (__syncthreads_or(later)) continue;
+    }
     if (tid == 0) missing = 0;
-    __syncthreads();
     if (tid < block) {
-      const int64_t s = first + tid;
-      int w = -1;
-      if (s < a.n_slots) {
+      win[tid] = -1;
+      const int64_t s = ((int64_t)blk << a.shift) + tid;
+      if (!SMALL && s < a.n_slots) {
         const int c = a.row_of[s];
-        if (c >= 0 && c < a.n && a.slots[c] == s) w = c;
-        if (w < 0) missing = 1;
+        if (c >= 0 && c < a.n && a.slots[c] == s) win[tid] = c;
       }
-      win[tid] = w;
     }
     __syncthreads();
-    float v[IT][8];
-    float mx = 0.f;
-#pragma unroll
-    for (int it = 0; it < IT; ++it) {
-      const int item = it * kThreads + tid, r = item / chunks, c = item - r * chunks;
-      const int w = item < items ? win[r] : -1;
-      if (w >= 0) {
-        load8(src + (int64_t)w * a.src_ld + c * 8, v[it]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[it][j] = 0.f;
-      }
+    if constexpr (SMALL) {
+      for (int i = tid; i < a.n; i += kThreads)
+        if (all[i] >= 0 && all[i] >> a.shift == blk) atomicMax(win + (all[i] & (block - 1)), i);
+      __syncthreads();
     }
-#pragma unroll
-    for (int it = 0; it < IT; ++it)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) mx = fmaxf(mx, fabsf(v[it][j]) < INFINITY ? fabsf(v[it][j]) : 0.f);
-    mx = wave_max(mx);
-    if ((tid & 63) == 0) red[tid >> 6] = mx;
-    __syncthreads();
-    mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    float* sp = a.scales[which] + (int64_t)blk * a.heads + g;
-    const float old = *sp;
-    const int was = old > 0.f ? (int)(__float_as_uint(old) >> 23) : 0;
-    int e = scale_byte(mx);
-    if (missing && was) e = max(e, min(was, kMaxScaleByte));
-    const float inv = pow2_byte(254 - e);
-#pragma unroll
-    for (int it = 0; it < IT; ++it) {
-      const int item = it * kThreads + tid, r = item / chunks, c = item - r * chunks;
-      if (item >= items || first + r >= a.n_slots) continue;
-      uint8_t* p = codes + (first + r) * a.ld + c * 8;
-      if (win[r] >= 0) {
-        float y[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = code_arg(v[it][j], inv);
-        *reinterpret_cast<u32x2*>(p) = u32x2{encode4(y[0], y[1], y[2], y[3]), encode4(y[4], y[5], y[6], y[7])};
-      } else if (!was) {
-        *reinterpret_cast<u32x2*>(p) = u32x2{0u, 0u};  // of an empty block: reads as zero before and after
-      } else if (e > was) {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(p);
-        float lo[4], hi[4];
-        decode4(w[0], lo);
-        decode4(w[1], hi);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          lo[j] = __builtin_amdgcn_ldexpf(lo[j], was - e);
-          hi[j] = __builtin_amdgcn_ldexpf(hi[j], was - e);
-        }
-        *reinterpret_cast<u32x2*>(p) = u32x2{encode4(lo[0], lo[1], lo[2], lo[3]), encode4(hi[0], hi[1], hi[2], hi[3])};
-      }
-    }
-    __syncthreads();  // every thread has read the old scale, win and red
-    if (tid == 0) *sp = pow2_byte(e);
+    store_block<T, IT>(a, which, g, blk, win, red, &missing);
+    __syncthreads();  // win, red and missing are free
   }
 }
 
@@ -220,15 +263,16 @@ __global__ __launch_bounds__(kThreads) void quant_load_kernel(const uint8_t* __r
   }
 }
 
-template <typename T>
-void store_items(const StoreArgs<T>& a, dim3 grid, int it, hipStream_t s) {
-  switch (it) {
-    case 1: hipLaunchKernelGGL((quant_store_kernel<T, 1>), grid, dim3(kThreads), 0, s, a); break;
-    case 2: hipLaunchKernelGGL((quant_store_kernel<T, 2>), grid, dim3(kThreads), 0, s, a); break;
-    case 4: hipLaunchKernelGGL((quant_store_kernel<T, 4>), grid, dim3(kThreads), 0, s, a); break;
-    case 8: hipLaunchKernelGGL((quant_store_kernel<T, 8>), grid, dim3(kThreads), 0, s, a); break;
-    default: hipLaunchKernelGGL((quant_store_kernel<T, 16>), grid, dim3(kThreads), 0, s, a); break;
-  }
+template <typename T, bool SMALL>
+void store_items(const StoreArgs<T>& a, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)((a.n + (1 << a.shift) - 1) >> a.shift) * 2 * a.heads));
+  const int items = (a.head_dim >> 3) << a.shift;
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, a); };
+  if (items <= kThreads) go(quant_store_kernel<T, 1, SMALL>);
+  else if (items <= 2 * kThreads) go(quant_store_kernel<T, 2, SMALL>);
+  else if (items <= 4 * kThreads) go(quant_store_kernel<T, 4, SMALL>);
+  else if (items <= 8 * kThreads) go(quant_store_kernel<T, 8, SMALL>);
+  else go(quant_store_kernel<T, 16, SMALL>);
 }
 
 template <typename T>
@@ -253,13 +297,14 @@ hipError_t store(const QuantPool& p, const void* k, const void* v, int64_t src_l
   a.heads = p.heads;
   a.head_dim = p.head_dim;
   a.shift = p.shift;
-  const unsigned wgs = (unsigned)((n + kThreads - 1) / kThreads);
-  hipLaunchKernelGGL(quant_clear_kernel, dim3(wgs), dim3(kThreads), 0, s, slots, n, p.n_slots, p.shift, row_of, last_of);
-  hipLaunchKernelGGL(quant_map_kernel, dim3(wgs), dim3(kThreads), 0, s, slots, n, p.n_slots, p.shift, row_of, last_of);
-  const int need = (((p.head_dim >> 3) << p.shift) + kThreads - 1) / kThreads;
-  int it = 1;
-  while (it < need) it *= 2;
-  store_items(a, dim3((unsigned)((n + (1 << p.shift) - 1) >> p.shift), (unsigned)(2 * p.heads)), it, s);
+  if (n <= kSmallRows) {
+    store_items<T, true>(a, s);
+    return hipGetLastError();
+  }
+  const dim3 wgs((unsigned)(((int64_t)n + kThreads - 1) / kThreads));
+  hipLaunchKernelGGL(quant_clear_kernel, wgs, dim3(kThreads), 0, s, slots, n, p.n_slots, p.shift, row_of, last_of);
+  hipLaunchKernelGGL(quant_map_kernel, wgs, dim3(kThreads), 0, s, slots, n, p.n_slots, p.shift, row_of, last_of);
+  store_items<T, false>(a, s);
   return hipGetLastError();
 }
 
