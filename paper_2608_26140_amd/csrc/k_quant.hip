@@ -14,18 +14,89 @@ typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32x2;
 constexpr int kThreads = 256;
 constexpr int kMaxBlock = 256;  // slots that share a scale, at most
 
-__device__ __forceinline__ void load8(const bf16* p, float (&v)[8]) {
-  const bf16x8 w = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(p));
-#pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = (float)w[j];
-}
-__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-  const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    v[j] = a[j];
-    v[4 + j] = b[j];
+// Eight consecutive elements as they lie in memory; none: zeros.
+template <typename T>
+struct Piece;
+template <>
+struct Piece<bf16> {
+  u32x4 w;
+  __device__ __forceinline__ void load(const bf16* p) { w = *reinterpret_cast<const u32x4*>(p); }
+  __device__ __forceinline__ void none() { w = u32x4{0u, 0u, 0u, 0u}; }
+  __device__ __forceinline__ float at(int j) const {
+    return __uint_as_float(j & 1 ? w[j >> 1] & 0xFFFF0000u : w[j >> 1] << 16);
   }
+  // the largest magnitude, infinities and NaN above all (their bits are), two
+  // elements at a time
+  __device__ __forceinline__ float top() const {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 m = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[j] & 0x7FFF7FFFu));
+    return __uint_as_float((uint32_t)(m[0] > m[1] ? m[0] : m[1]) << 16);
+  }
+  // codes of finite elements within the scale's range
+  __device__ __forceinline__ u32x2 encode(float scale) const {
+    u32x2 c;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) c[j] = pair(w[2 * j], scale) | pair(w[2 * j + 1], scale) << 16;
+    return c;
+  }
+  // two codes in the low half (the form that writes the high half of what is
+  // there is not used: the compiler gives it the first form's operand)
+  static __device__ __forceinline__ uint32_t pair(uint32_t x, float scale) {
+    typedef short i16x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const i16x2 none = {0, 0};
+    return __builtin_bit_cast(
+        uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(none, __builtin_bit_cast(bf16x2, x), scale, false));
+  }
+};
+template <>
+struct Piece<float> {
+  f32x4 v[2];
+  __device__ __forceinline__ void load(const float* p) {
+    v[0] = reinterpret_cast<const f32x4*>(p)[0];
+    v[1] = reinterpret_cast<const f32x4*>(p)[1];
+  }
+  __device__ __forceinline__ void none() { v[0] = v[1] = f32x4{0.f, 0.f, 0.f, 0.f}; }
+  __device__ __forceinline__ float at(int j) const { return v[j >> 2][j & 3]; }
+  __device__ __forceinline__ float top() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(at(j)) & 0x7FFFFFFFu);
+    return __uint_as_float(m);
+  }
+  __device__ __forceinline__ u32x2 encode(float scale) const {
+    const float inv = pow2_byte(254 - (int)(__float_as_uint(scale) >> 23));
+    return u32x2{encode4(v[0][0] * inv, v[0][1] * inv, v[0][2] * inv, v[0][3] * inv),
+                 encode4(v[1][0] * inv, v[1][1] * inv, v[1][2] * inv, v[1][3] * inv)};
+  }
+};
+// The largest finite magnitude, and codes of any elements.
+template <typename T>
+__device__ __forceinline__ float finite_top(const Piece<T>& x) {
+  float m = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(x.at(j)) < INFINITY ? fabsf(x.at(j)) : 0.f);
+  return m;
+}
+template <typename T>
+__device__ __forceinline__ u32x2 encode_any(const Piece<T>& x, float inv) {
+  float y[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) y[j] = code_arg(x.at(j), inv);
+  return u32x2{encode4(y[0], y[1], y[2], y[3]), encode4(y[4], y[5], y[6], y[7])};
+}
+
+// Maximum of non-negative bit patterns (infinities and NaN above all) over the
+// workgroup.
+__device__ __forceinline__ float group_top(float m, uint32_t* red) {
+  uint32_t u = __float_as_uint(m);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) u = max(u, (uint32_t)__shfl_xor((int)u, o));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = u;
+  __syncthreads();
+  return __uint_as_float(max(max(red[0], red[1]), max(red[2], red[3])));
 }
 
 // ============================================================================
@@ -36,11 +107,10 @@ __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
 // found through a map from its slots to the last row of each.
 //   Up to kSmallRows rows every workgroup reads all the call's slots and makes
 // its block's map in LDS: one launch.
-//   Beyond, the map lies in the workspace: a launch marks the slots that are
-// named (the entries of the others stay what they were), the next leaves the
-// last row of each, and the one that quantises takes an entry for a row of
-// this call only where that row's slot is the entry's own, which no stale entry
-// can pretend.
+//   Beyond, a launch of its own leaves the map in the workspace.  Entries of
+// slots that are not named stay what they were: the launch that quantises takes
+// an entry for a row of this call only where that row's slot is the entry's
+// own, which no stale entry can pretend.
 // Bound by HBM: 3 bytes an element of bf16.  Workgroups of neighbouring heads
 // are neighbours in the grid, so that whole rows are read and written together.
 // ============================================================================
@@ -63,77 +133,85 @@ __device__ __forceinline__ bool ends_run(const int32_t* slots, int i, int n, int
   return i + 1 == n || (slots[i + 1] >> shift) != (slots[i] >> shift);
 }
 
-__global__ __launch_bounds__(kThreads) void quant_clear_kernel(const int32_t* __restrict__ slots, int n,
-                                                               int64_t n_slots, int shift, int32_t* __restrict__ row_of,
-                                                               int32_t* __restrict__ last_of) {
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= n) return;
-  const int s = slots[i];
-  if (s < 0 || s >= n_slots) return;
-  row_of[s] = -1;
-  if (ends_run(slots, (int)i, n, shift)) last_of[s >> shift] = -1;
+// Leaves the last row of every slot that a call names, and of every block, in
+// tables of any earlier contents.  A row puts itself into its entry; where it
+// takes out another row of this call it offers that row to the entry again, as
+// a maximum.  Whoever takes the last row out puts it back, so it stays.  (Two
+// launches, one that clears the entries and one that raises them, took 9.5 us
+// for 8192 rows where this takes 4.6.)  64 rows at one entry of last_of would
+// queue for it, so only the ends of runs of rows of one block go there.
+template <typename F>
+__device__ __forceinline__ void keep_last(int32_t* entry, int i, F is_row) {
+  const int other = atomicExch(entry, i);
+  if (other != i && is_row(other)) atomicMax(entry, other);
 }
-// (64 rows raising one entry of last_of would queue for it: 7372 rows took 16
-// us so, the ends of runs alone RRR)
 __global__ __launch_bounds__(kThreads) void quant_map_kernel(const int32_t* __restrict__ slots, int n, int64_t n_slots,
                                                              int shift, int32_t* __restrict__ row_of,
                                                              int32_t* __restrict__ last_of) {
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= n) return;
-  const int s = slots[i];
+  const int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (at >= n) return;
+  const int i = (int)at, s = slots[i];
   if (s < 0 || s >= n_slots) return;
-  atomicMax(row_of + s, (int)i);
-  if (ends_run(slots, (int)i, n, shift)) atomicMax(last_of + (s >> shift), (int)i);
+  keep_last(row_of + s, i, [&](int j) { return j >= 0 && j < n && slots[j] == s; });
+  if (ends_run(slots, i, n, shift))
+    keep_last(last_of + (s >> shift), i, [&](int j) { return j >= 0 && j < n && slots[j] >> shift == s >> shift; });
 }
 
 // Quantises one block and head from its map win (LDS): the row stored at each
 // slot, -1 where none is.  IT: 8-element pieces of the block for each thread.
 template <typename T, int IT>
 __device__ __forceinline__ void store_block(const StoreArgs<T>& a, int which, int g, int blk, const int32_t* win,
-                                            float* red, int* missing) {
+                                            uint32_t* red, bool missing) {
   const int tid = threadIdx.x;
   const int64_t first = (int64_t)blk << a.shift;
-  const int chunks = a.head_dim >> 3, items = chunks << a.shift;
+  // pieces tid, tid + kThreads, ..: piece c of the block's row r
+  const int chunks = a.head_dim >> 3, rows = 1 << a.shift;
+  const int dr = kThreads / chunks, dc = kThreads - dr * chunks, r0 = tid / chunks, c0 = tid - r0 * chunks;
+  auto next = [&](int& r, int& c) {
+    r += dr;
+    c += dc;
+    if (c >= chunks) {
+      c -= chunks;
+      ++r;
+    }
+  };
   const T* src = a.src[which] + g * a.head_dim;
   uint8_t* codes = a.codes[which] + g * a.head_dim;
   float* sp = a.scales[which] + (int64_t)blk * a.heads + g;
   const float old = *sp;
-  float v[IT][8];
+  Piece<T> v[IT];
   float mx = 0.f;
+  int r = r0, c = c0;
 #pragma unroll
-  for (int it = 0; it < IT; ++it) {
-    const int item = it * kThreads + tid, r = item / chunks, c = item - r * chunks;
-    const int w = item < items ? win[r] : -1;
-    if (w >= 0) {
-      load8(src + (int64_t)w * a.src_ld + c * 8, v[it]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[it][j] = 0.f;
-    }
+  for (int it = 0; it < IT; ++it, next(r, c)) {
+    const int w = r < rows ? win[r] : -1;
+    if (w >= 0) v[it].load(src + (int64_t)w * a.src_ld + c * 8);
+    else v[it].none();
   }
-  if (tid < 1 << a.shift && first + tid < a.n_slots && win[tid] < 0) *missing = 1;
 #pragma unroll
-  for (int it = 0; it < IT; ++it)
+  for (int it = 0; it < IT; ++it) mx = __uint_as_float(max(__float_as_uint(mx), __float_as_uint(v[it].top())));
+  mx = group_top(mx, red);
+  // an element that is not finite, or past the largest scale's range: the
+  // careful way, which no ordinary block takes
+  const bool odd = !(mx <= kMaxCode * pow2_byte(kMaxScaleByte));
+  if (odd) {
+    mx = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) mx = fmaxf(mx, fabsf(v[it][j]) < INFINITY ? fabsf(v[it][j]) : 0.f);
-  mx = wave_max(mx);
-  if ((tid & 63) == 0) red[tid >> 6] = mx;
-  __syncthreads();
-  mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    for (int it = 0; it < IT; ++it) mx = fmaxf(mx, finite_top(v[it]));
+    __syncthreads();
+    mx = group_top(mx, red);
+  }
   const int was = old > 0.f ? (int)(__float_as_uint(old) >> 23) : 0;
   int e = scale_byte(mx);
-  if (*missing && was) e = max(e, min(was, kMaxScaleByte));
-  const float inv = pow2_byte(254 - e);
+  if (missing && was) e = max(e, min(was, kMaxScaleByte));
+  r = r0;
+  c = c0;
 #pragma unroll
-  for (int it = 0; it < IT; ++it) {
-    const int item = it * kThreads + tid, r = item / chunks, c = item - r * chunks;
-    if (item >= items || first + r >= a.n_slots) continue;
+  for (int it = 0; it < IT; ++it, next(r, c)) {
+    if (r >= rows || first + r >= a.n_slots) continue;
     uint8_t* p = codes + (first + r) * a.ld + c * 8;
     if (win[r] >= 0) {
-      float y[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = code_arg(v[it][j], inv);
-      *reinterpret_cast<u32x2*>(p) = u32x2{encode4(y[0], y[1], y[2], y[3]), encode4(y[4], y[5], y[6], y[7])};
+      *reinterpret_cast<u32x2*>(p) = odd ? encode_any(v[it], pow2_byte(254 - e)) : v[it].encode(pow2_byte(e));
     } else if (!was) {
       *reinterpret_cast<u32x2*>(p) = u32x2{0u, 0u};  // of an empty block: reads as zero before and after
     } else if (e > was) {
@@ -157,8 +235,8 @@ __global__ __launch_bounds__(kThreads) void quant_store_kernel(StoreArgs<T> a) {
   __shared__ int32_t all[SMALL ? kSmallRows : 1];  // the call's slots, -1 those that are not there
   __shared__ int32_t win[kMaxBlock];
   __shared__ int32_t found[kMaxBlock];  // rows of this workgroup's that may be their block's last
-  __shared__ int n_found, missing;
-  __shared__ float red[kThreads / 64];
+  __shared__ int n_found;
+  __shared__ uint32_t red[kThreads / 64];
   const int tid = threadIdx.x, block = 1 << a.shift;
   const unsigned chunk = blockIdx.x / (2u * a.heads), h = blockIdx.x - chunk * (2u * a.heads);
   const int which = (int)h >= a.heads, g = (int)h - which * a.heads;
@@ -189,7 +267,6 @@ __global__ __launch_bounds__(kThreads) void quant_store_kernel(StoreArgs<T> a) {
       for (int i = row + 1 + tid; i < a.n; i += kThreads) later |= all[i] >= 0 && all[i] >> a.shift == blk;
       if (__syncthreads_or(later)) continue;
     }
-    if (tid == 0) missing = 0;
     if (tid < block) {
       win[tid] = -1;
       const int64_t s = ((int64_t)blk << a.shift) + tid;
@@ -204,8 +281,10 @@ __global__ __launch_bounds__(kThreads) void quant_store_kernel(StoreArgs<T> a) {
         if (all[i] >= 0 && all[i] >> a.shift == blk) atomicMax(win + (all[i] & (block - 1)), i);
       __syncthreads();
     }
-    store_block<T, IT>(a, which, g, blk, win, red, &missing);
-    __syncthreads();  // win, red and missing are free
+    const int64_t s = ((int64_t)blk << a.shift) + tid;
+    const bool missing = __syncthreads_or(tid < block && s < a.n_slots && win[tid] < 0);
+    store_block<T, IT>(a, which, g, blk, win, red, missing);
+    __syncthreads();  // win and red are free
   }
 }
 
@@ -265,7 +344,7 @@ __global__ __launch_bounds__(kThreads) void quant_load_kernel(const uint8_t* __r
 
 template <typename T, bool SMALL>
 void store_items(const StoreArgs<T>& a, hipStream_t s) {
-  const dim3 grid((unsigned)((int64_t)((a.n + (1 << a.shift) - 1) >> a.shift) * 2 * a.heads));
+  const dim3 grid((unsigned)((((int64_t)a.n + (1 << a.shift) - 1) >> a.shift) * 2 * a.heads));
   const int items = (a.head_dim >> 3) << a.shift;
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, a); };
   if (items <= kThreads) go(quant_store_kernel<T, 1, SMALL>);
@@ -301,9 +380,8 @@ hipError_t store(const QuantPool& p, const void* k, const void* v, int64_t src_l
     store_items<T, true>(a, s);
     return hipGetLastError();
   }
-  const dim3 wgs((unsigned)(((int64_t)n + kThreads - 1) / kThreads));
-  hipLaunchKernelGGL(quant_clear_kernel, wgs, dim3(kThreads), 0, s, slots, n, p.n_slots, p.shift, row_of, last_of);
-  hipLaunchKernelGGL(quant_map_kernel, wgs, dim3(kThreads), 0, s, slots, n, p.n_slots, p.shift, row_of, last_of);
+  hipLaunchKernelGGL(quant_map_kernel, dim3((unsigned)(((int64_t)n + kThreads - 1) / kThreads)), dim3(kThreads), 0, s,
+                     slots, n, p.n_slots, p.shift, row_of, last_of);
   store_items<T, false>(a, s);
   return hipGetLastError();
 }
