@@ -542,6 +542,28 @@ acache_status acache_quant_attention(const acache_dims* dims, const acache_ragge
  * invalid dims or an invalid pool (its pointers are not looked at). */
 size_t acache_quant_workspace_size(const acache_dims* dims, int32_t max_rows, const acache_quant_pool* pool);
 
+/* acache_quant_layer_recompute — acache_layer_recompute over an 8-bit cache:
+ * the rows' fresh K and V are stored as acache_quant_store does, and the
+ * attention reads the cache as acache_quant_attention does.  With `score`
+ * set, the affix keys of Eq. 4 are the cache's values; the score makes its own
+ * pass over them (affix_keys_known is not used).  write_slots, read_slots and
+ * the other arguments, shapes and errors are those of acache_layer_recompute;
+ * bf16 only, n_slots * ld < 2^31.  A decode step (Section 4.3) is this call
+ * with the block's rows, their slots and the refresh's read_slots.  ws: at
+ * least acache_quant_layer_workspace_size(dims, rows, batch, L, pool) bytes
+ * (a workspace of more rows, requests and affix keys serves smaller calls). */
+acache_status acache_quant_layer_recompute(const acache_dims* dims, const acache_layer_weights* w,
+                                           const acache_ragged* rg, void* x, const int32_t* pos,
+                                           const int32_t* write_slots, const int32_t* read_slots,
+                                           const acache_quant_pool* pool, const acache_score_args* score, void* ws,
+                                           size_t ws_bytes, hipStream_t stream);
+
+/* Workspace bytes of acache_quant_layer_recompute for up to max_rows rows,
+ * `batch` requests and affix length affix_len (0 when no scoring); 0 for
+ * invalid dims, dims that are not bf16, or an invalid pool. */
+size_t acache_quant_layer_workspace_size(const acache_dims* dims, int32_t max_rows, int32_t batch, int32_t affix_len,
+                                         const acache_quant_pool* pool);
+
 /* ---------------------------------------------------------------------------
  * Measurement hook (benchmarks only).  While armed for kernel `kernel`,
  * every launch of that kernel by any entry point records starts[i] before

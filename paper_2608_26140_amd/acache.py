@@ -105,6 +105,8 @@ def _load():
         "acache_quant_store": [ctypes.POINTER(Dims), QP, P, P, I64, I32, P, P, SZ, P],
         "acache_quant_load": [ctypes.POINTER(Dims), QP, P, I32, P, P, I64, P],
         "acache_quant_attention": [ctypes.POINTER(Dims), ctypes.POINTER(Ragged), P, P, QP, P, P, P, SZ, P],
+        "acache_quant_layer_recompute": [ctypes.POINTER(Dims), ctypes.POINTER(LayerWeights), ctypes.POINTER(Ragged),
+                                         P, P, P, P, QP, ctypes.POINTER(ScoreArgs), P, SZ, P],
     })
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -114,6 +116,8 @@ def _load():
     lib.acache_workspace_size.restype = ctypes.c_size_t
     lib.acache_quant_workspace_size.argtypes = [ctypes.POINTER(Dims), I32, QP]
     lib.acache_quant_workspace_size.restype = ctypes.c_size_t
+    lib.acache_quant_layer_workspace_size.argtypes = [ctypes.POINTER(Dims), I32, I32, I32, QP]
+    lib.acache_quant_layer_workspace_size.restype = ctypes.c_size_t
     lib.acache_status_string.argtypes = [ctypes.c_int32]
     lib.acache_status_string.restype = ctypes.c_char_p
     lib.acache_version.restype = ctypes.c_int32
@@ -652,6 +656,45 @@ def acache_quant_attention(dims: Dims, cu_rows, cu_keys, q: torch.Tensor, read_s
         ctypes.byref(dims), ctypes.byref(rg), q.data_ptr(), read_slots.data_ptr(), pool.ref, out.data_ptr(),
         _ptr(lse), _ptr(ws), 0 if ws is None else ws.nbytes, _stream(stream)))
     return out
+
+
+def acache_quant_layer_workspace_size(dims: Dims, max_rows: int, batch: int, affix_len: int, pool: QuantPool) -> int:
+    n = lib.acache_quant_layer_workspace_size(ctypes.byref(dims), max_rows, batch, affix_len, pool.ref)
+    if n == 0:
+        raise AcacheError("acache_quant_layer_workspace_size", 2, "invalid dims or pool")
+    return n
+
+
+def quant_layer_workspace(dims: Dims, max_rows: int, batch: int, affix_len: int, pool: QuantPool) -> torch.Tensor:
+    """Workspace for acache_quant_layer_recompute of up to max_rows rows."""
+    return torch.empty(acache_quant_layer_workspace_size(dims, max_rows, batch, affix_len, pool), dtype=torch.uint8,
+                       device=pool.device)
+
+
+def acache_quant_layer_recompute(dims: Dims, weights, cu_rows, cu_keys, x: torch.Tensor, pos: torch.Tensor,
+                                 write_slots: torch.Tensor, read_slots: torch.Tensor, pool: QuantPool,
+                                 ws: torch.Tensor, score: Optional[dict] = None, stream=None):
+    """acache_layer_recompute over an 8-bit cache, in place on x (ws from
+    quant_layer_workspace; score as there, affix_key_begin unused)."""
+    for t, n in ((pos, "pos"), (write_slots, "write_slots"), (read_slots, "read_slots")):
+        _dev_i32(t, n)
+    rows = int(cu_rows[-1])
+    if x.dtype != torch_dtype(dims) or not x.is_contiguous() or x.numel() < rows * dims.d_model:
+        raise TypeError("x must be a contiguous tensor of dims' type with [rows, d_model] values")
+    if pos.numel() < rows or write_slots.numel() < rows or read_slots.numel() < int(cu_keys[-1]):
+        raise ValueError("pos and write_slots hold cu_rows[-1] values, read_slots cu_keys[-1]")
+    _quant_check(dims, pool, x, pos, write_slots, read_slots, ws)
+    lw = weights if isinstance(weights, LayerWeights) else layer_weights(weights)
+    rg, keep = _ragged(cu_rows, cu_keys)
+    sa = None
+    if score is not None:
+        cq = _i32(score["cu_q"])
+        sa = ScoreArgs(score["q_rows"].data_ptr(), cq, score["affix_slots"].data_ptr(), score["affix_slots"].numel(),
+                       score.get("norm", ACACHE_NORM_AFFIX), score["scores"].data_ptr(), int(score.get("init", 0)))
+    _check("acache_quant_layer_recompute", lib.acache_quant_layer_recompute(
+        ctypes.byref(dims), ctypes.byref(lw), ctypes.byref(rg), x.data_ptr(), pos.data_ptr(), write_slots.data_ptr(),
+        read_slots.data_ptr(), pool.ref, ctypes.byref(sa) if sa is not None else None, ws.data_ptr(), ws.nbytes,
+        _stream(stream)))
 
 
 # ---------------------------------------------------------------------------- measurement hook

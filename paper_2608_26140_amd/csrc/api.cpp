@@ -1014,4 +1014,109 @@ acache_status acache_quant_attention(const acache_dims* dims, const acache_ragge
   return ACACHE_OK;
 }
 
+// The 8-bit layer's workspace: a layer's, then the fresh K and V rows, the
+// indices 0, 1, .. that address them and the affix keys, those keys, and the
+// store's map.
+struct QuantWsPlan {
+  size_t k, v, iota, affix_k, map, total;
+};
+static QuantWsPlan plan_quant_ws(const acache_dims* d, int rows, int batch, int L, const QuantPool& p) {
+  QuantWsPlan w;
+  size_t off = align_up(plan_ws(d, rows, batch, L).total);
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off += align_up(bytes);
+    return at;
+  };
+  const size_t row = (size_t)p.heads * p.head_dim * 2;
+  w.k = take((size_t)rows * row);
+  w.v = take((size_t)rows * row);
+  w.iota = take((size_t)std::max(rows, L) * sizeof(int32_t));
+  w.affix_k = take((size_t)L * row);
+  w.map = take(quant_map_bytes(p.n_slots, p.shift));
+  w.total = off;
+  return w;
+}
+
+size_t acache_quant_layer_workspace_size(const acache_dims* dims, int32_t max_rows, int32_t batch, int32_t affix_len,
+                                         const acache_quant_pool* pool) {
+  QuantPool p;
+  if (check_quant_pool(dims, pool, p) != ACACHE_OK || dims->dtype != ACACHE_BF16) return 0;
+  if (max_rows < 0 || batch < 0 || affix_len < 0) return 0;
+  return plan_quant_ws(dims, max_rows, batch, affix_len, p).total;
+}
+
+acache_status acache_quant_layer_recompute(const acache_dims* dims, const acache_layer_weights* w,
+                                           const acache_ragged* rg, void* x, const int32_t* pos,
+                                           const int32_t* write_slots, const int32_t* read_slots,
+                                           const acache_quant_pool* pool, const acache_score_args* score, void* ws,
+                                           size_t ws_bytes, hipStream_t stream) {
+  acache_status st = check_layer_dims(dims);
+  if (st != ACACHE_OK) return st;
+  CHECK(dims->dtype == ACACHE_BF16, ACACHE_ERR_UNSUPPORTED);
+  QuantPool p;
+  st = check_quant_pool(dims, pool, p);
+  if (st != ACACHE_OK) return st;
+  Ragged r;
+  st = make_ragged(rg, r);
+  if (st != ACACHE_OK) return st;
+  const int M = r.cu_rows[r.batch];
+  if (M == 0) return ACACHE_OK;
+  CHECK(w && x && pos && write_slots && read_slots, ACACHE_ERR_NULL);
+  CHECK(w->attn_norm && w->w_qkv && w->w_o && w->mlp_norm && w->w_gate_up && w->w_down, ACACHE_ERR_NULL);
+  st = check_quant_buffers(p);
+  if (st != ACACHE_OK) return st;
+  const int d = dims->d_model, H = dims->n_heads, Hkv = dims->n_kv_heads, dh = dims->head_dim, F = dims->d_ff;
+  const int hq = H * dh, hkv = Hkv * dh, nqkv = (H + 2 * Hkv) * dh;
+  CHECK(p.n_slots > 0, ACACHE_ERR_SHAPE);
+  CHECK(p.n_slots * p.ld < ((int64_t)1 << 31), ACACHE_ERR_UNSUPPORTED);  // 32-bit offsets
+  CHECK((int64_t)M * std::max({d, hq, hkv, F}) < ((int64_t)1 << 31), ACACHE_ERR_UNSUPPORTED);
+  CHECK((int64_t)std::max({nqkv, 2 * F, d}) * std::max({d, hq, F}) < ((int64_t)1 << 31), ACACHE_ERR_UNSUPPORTED);
+  CHECK(aligned16(x), ACACHE_ERR_ALIGN);
+  CHECK(aligned16(w->attn_norm) && aligned16(w->w_qkv) && aligned16(w->w_o) && aligned16(w->mlp_norm) &&
+            aligned16(w->w_gate_up) && aligned16(w->w_down),
+        ACACHE_ERR_ALIGN);
+  int L = 0;
+  if (score) {
+    L = score->affix_len;
+    CHECK(L >= 0 && L <= 65536, ACACHE_ERR_SHAPE);
+    CHECK(score->norm == ACACHE_NORM_AFFIX || score->norm == ACACHE_NORM_FULL, ACACHE_ERR_UNSUPPORTED);
+    st = check_cu(score->cu_q, r.batch);
+    if (st != ACACHE_OK) return st;
+    CHECK(score->cu_q[r.batch] <= M, ACACHE_ERR_SHAPE);
+    if (L > 0 && score->cu_q[r.batch] > 0) CHECK(score->q_rows && score->affix_slots && score->scores, ACACHE_ERR_NULL);
+  }
+  const WsPlan lp = plan_ws(dims, M, r.batch, L);
+  const QuantWsPlan qp = plan_quant_ws(dims, M, r.batch, L, p);
+  CHECK(ws && ws_bytes >= qp.total && aligned16(ws), ACACHE_ERR_WORKSPACE);
+  const bool probe = score && L > 0 && score->cu_q[r.batch] > 0;
+  void* y = at<char>(ws, lp.y);
+  void* q = at<char>(ws, lp.q);
+  void* o = at<char>(ws, lp.o);
+  float* part = at<float>(ws, lp.part);
+  float* lse = (probe && score->norm == ACACHE_NORM_FULL) ? at<float>(ws, lp.lse) : nullptr;
+  int32_t* iota = at<int32_t>(ws, qp.iota);
+  void* k_rows = at<char>(ws, qp.k);
+  void* v_rows = at<char>(ws, qp.v);
+
+  LAUNCH(launch_iota(iota, std::max(M, probe ? L : 0), stream));
+  st = run_qkv_bf16(dims, w, M, x, y, q, pos, iota, k_rows, v_rows, hkv, M, part, at<float>(ws, lp.rope), stream);
+  if (st != ACACHE_OK) return st;
+  LAUNCH_T(ACACHE_K_SCATTER, stream,
+           launch_quant_store(ACACHE_BF16, p, k_rows, v_rows, hkv, M, write_slots, at<int32_t>(ws, qp.map), stream));
+  // the part region is idle between the QKV fixup and the O projection
+  LAUNCH_T(ACACHE_K_ATTENTION, stream,
+           launch_quant_attention(r, H, p, q, read_slots, o, lse, part, lp.part_bytes, stream));
+  if (probe) {
+    void* affix_k = at<char>(ws, qp.affix_k);
+    LAUNCH_T(ACACHE_K_GATHER, stream,
+             launch_quant_load(ACACHE_BF16, p, score->affix_slots, L, affix_k, nullptr, hkv, stream));
+    st = run_score(dims, r.batch, score->cu_q, q, hq, M, score->q_rows, affix_k, hkv, L, iota, L, score->norm, lse,
+                   score->scores, at<float>(ws, lp.lse_aff), at<float>(ws, lp.colsum), lp.colsum_bytes, score->init,
+                   stream);
+    if (st != ACACHE_OK) return st;
+  }
+  return run_out_mlp_bf16(dims, w, M, x, y, o, at<char>(ws, lp.h), part, stream);
+}
+
 }  // extern "C"

@@ -159,6 +159,7 @@ hipError_t launch_quant_store(acache_dtype dt, const QuantPool& p, const void* k
 // k or v may be null (not read back)
 hipError_t launch_quant_load(acache_dtype dt, const QuantPool& p, const int32_t* slots, int n, void* k, void* v,
                              int64_t dst_ld, hipStream_t s);
+hipError_t launch_iota(int32_t* out, int n, hipStream_t s);  // 0, 1, .., n - 1
 // part / part_bytes: optional space for key splits; quant_attention_part_bytes
 // of the most (row, head) pairs serves every smaller call.
 size_t quant_attention_part_bytes(int64_t pairs);

@@ -342,6 +342,11 @@ __global__ __launch_bounds__(kThreads) void quant_load_kernel(const uint8_t* __r
   }
 }
 
+__global__ __launch_bounds__(kThreads) void iota_kernel(int32_t* out, int n) {
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i < n) out[i] = (int32_t)i;
+}
+
 template <typename T, bool SMALL>
 void store_items(const StoreArgs<T>& a, hipStream_t s) {
   const dim3 grid((unsigned)((((int64_t)a.n + (1 << a.shift) - 1) >> a.shift) * 2 * a.heads));
@@ -390,6 +395,11 @@ hipError_t store(const QuantPool& p, const void* k, const void* v, int64_t src_l
 
 size_t quant_map_bytes(int64_t n_slots, int shift) {
   return (size_t)(n_slots + ((n_slots + (1 << shift) - 1) >> shift)) * sizeof(int32_t);
+}
+
+hipError_t launch_iota(int32_t* out, int n, hipStream_t s) {
+  hipLaunchKernelGGL(iota_kernel, dim3((unsigned)(((int64_t)n + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, out, n);
+  return hipGetLastError();
 }
 
 hipError_t launch_quant_store(acache_dtype dt, const QuantPool& p, const void* k, const void* v, int64_t src_ld, int n,

@@ -61,16 +61,30 @@ class AffixBatch:
     request a private block table of ceil(R / bs) blocks, grown when a call
     needs more rows and given back by release_private().  The pools hold
     enough blocks for the largest R the batch is built for (max_rows, else
-    S: full recomputation)."""
+    S: full recomputation).
+
+    quant_block: the caches are 8-bit (A.QuantPool, one per layer in
+    ``caches``; k_pools and v_pools are empty), with a scale for every
+    quant_block slots and KV head; bf16 models.  The affix and each request's
+    private slots then begin on a scale's block (the paged plan's block_size
+    has to be a multiple of quant_block), so that no request's entries share a
+    scale with another's."""
 
     def __init__(self, model: Model, seq_len: int, affix_begin: int, affix_len: int, mask_begin: int,
                  mask_len: int, batch: int, x_src: torch.Tensor, remap: Optional[torch.Tensor] = None,
                  private_stride: Optional[int] = None, max_rows: Optional[int] = None, device="cuda",
-                 block_size: Optional[int] = None):
+                 block_size: Optional[int] = None, quant_block: Optional[int] = None):
+        if quant_block and model.dims.dtype != A.ACACHE_BF16:
+            raise ValueError("8-bit caches need a bf16 model")
+        if quant_block and block_size and block_size % quant_block:
+            raise ValueError("block_size must be a multiple of quant_block")
         self.model = model
         self.S, self.ab, self.L = seq_len, affix_begin, affix_len
         self.mb, self.G, self.B = mask_begin, mask_len, batch
         self.stride = seq_len if private_stride is None else private_stride
+        self.private_base = affix_len
+        if quant_block:
+            self.stride, self.private_base = (-(-n // quant_block) * quant_block for n in (self.stride, affix_len))
         self.x_src = x_src
         self.remap = remap
         self.device = device
@@ -89,13 +103,20 @@ class AffixBatch:
                                          + j % block_size)
         else:
             self.pages = None
-            self.n_slots = affix_len + batch * self.stride
+            self.n_slots = self.private_base + batch * self.stride
             self.affix_slots = torch.arange(affix_len, dtype=torch.int32, device=device)
-        shape = (self.n_slots, model.kv_width)
-        self.k_pools = [torch.zeros(shape, dtype=model.dtype, device=device) for _ in range(model.n_layers)]
-        self.v_pools = [torch.zeros(shape, dtype=model.dtype, device=device) for _ in range(model.n_layers)]
-        self.ws = A.workspace(model.dims, batch * r_max, batch, affix_len, device)
-        self.layout = A.Layout(seq_len, affix_begin, affix_len, mask_begin, mask_len, 0, affix_len, self.stride)
+        self.quant_block = quant_block
+        if quant_block:
+            self.caches = [A.quant_pool(model.dims, self.n_slots, quant_block, device) for _ in range(model.n_layers)]
+            self.k_pools, self.v_pools = [], []
+            self.ws = A.quant_layer_workspace(model.dims, batch * r_max, batch, affix_len, self.caches[0])
+        else:
+            shape = (self.n_slots, model.kv_width)
+            self.caches = []
+            self.k_pools = [torch.zeros(shape, dtype=model.dtype, device=device) for _ in range(model.n_layers)]
+            self.v_pools = [torch.zeros(shape, dtype=model.dtype, device=device) for _ in range(model.n_layers)]
+            self.ws = A.workspace(model.dims, batch * r_max, batch, affix_len, device)
+        self.layout = A.Layout(seq_len, affix_begin, affix_len, mask_begin, mask_len, 0, self.private_base, self.stride)
 
     def _i32(self, a) -> torch.Tensor:
         return torch.from_numpy(np.ascontiguousarray(np.asarray(a), dtype=np.int32)).to(self.device)
@@ -123,13 +144,16 @@ class AffixBatch:
         """[B, R] slot of request b's rank-i recomputed row (host copy)."""
         i = np.arange(R)
         if self.pages is None:
-            return self.L + np.arange(self.B)[:, None] * self.stride + i[None, :]
+            return self.private_base + np.arange(self.B)[:, None] * self.stride + i[None, :]
         _, nb = self.private_table(R)
         tbl = np.asarray(self._table_host, dtype=np.int64).reshape(self.B, nb)
         return tbl[:, i // self.bs] * self.bs + i % self.bs
 
     def kv_bytes(self, blocks: int) -> int:
         """Bytes of K and V over every layer held by `blocks` blocks."""
+        if self.quant_block:  # codes and scales
+            scales = self.bs // self.quant_block * self.model.dims.n_kv_heads * 4
+            return blocks * (self.bs * self.model.kv_width + scales) * 2 * self.model.n_layers
         return blocks * self.bs * self.model.kv_width * 2 * self.model.n_layers * self.k_pools[0].element_size()
 
     # ------------------------------------------------------------------ pieces
@@ -165,6 +189,17 @@ class AffixBatch:
         per = max(1, ((1 << 31) - 1) // max(1, R * widest))
         return [(b0, min(self.B, b0 + per)) for b0 in range(0, self.B, per)]
 
+    def recompute_layer(self, n: int, cu_rows, cu_keys, x: torch.Tensor, pos: torch.Tensor, write_slots: torch.Tensor,
+                        read_slots: torch.Tensor, score: Optional[dict] = None, stream=None):
+        """One layer call over this batch's cache of layer n."""
+        dims, lw = self.model.dims, self.model.lw[n]
+        if self.quant_block:
+            A.acache_quant_layer_recompute(dims, lw, cu_rows, cu_keys, x, pos, write_slots, read_slots, self.caches[n],
+                                           self.ws, score=score, stream=stream)
+        else:
+            A.acache_layer_recompute(dims, lw, cu_rows, cu_keys, x, pos, write_slots, read_slots, self.k_pools[n],
+                                     self.v_pools[n], self.ws, score=score, stream=stream)
+
     def run_layers(self, x: torch.Tensor, m: dict, k: int, score: Optional[dict] = None,
                    drop_non_anchor: bool = False, upto: Optional[int] = None, score_last_only: bool = False,
                    stream=None, layer_hook: Optional[Callable[[int, torch.Tensor], None]] = None):
@@ -172,7 +207,8 @@ class AffixBatch:
         Section 5.3): their write slots serve as the read slots, R keys per
         request, and the non-anchor affix entries are never read.
         score_last_only: the last layer only adds its score (acache_layer_score)
-        and x is left at the last layer's input.
+        and x is left at the last layer's input (8-bit caches: the last layer
+        runs whole).
         layer_hook(n, x): called on the host before layer n's launches are
         issued (x then holds layer n's input in stream order), and once more
         with n = the number of layers run after the last one; for inspection,
@@ -186,18 +222,21 @@ class AffixBatch:
         for n in range(n_run):
             if layer_hook is not None:
                 layer_hook(n, x)
-            layer = A.acache_layer_recompute
-            if score is not None and score_last_only and n == self.model.n_layers - 1:
-                layer = A.acache_layer_score
+            score_only = (score is not None and score_last_only and n == self.model.n_layers - 1
+                          and not self.quant_block)
             for b0, b1 in groups:
                 nb = b1 - b0
                 cu_rows = [b * R for b in range(nb + 1)]
                 cu_keys = [b * nk for b in range(nb + 1)]
                 rows = slice(b0 * R, b1 * R)
                 sc = score if score is None or n == 0 else dict(score, init=0)
-                layer(self.model.dims, self.model.lw[n], cu_rows, cu_keys, x[rows], m["row_pos"][rows],
-                      m["write_slots"][rows], read[b0 * nk:b1 * nk], self.k_pools[n], self.v_pools[n], self.ws,
-                      score=sc, stream=stream)
+                if score_only:
+                    A.acache_layer_score(self.model.dims, self.model.lw[n], cu_rows, cu_keys, x[rows],
+                                         m["row_pos"][rows], m["write_slots"][rows], read[b0 * nk:b1 * nk],
+                                         self.k_pools[n], self.v_pools[n], self.ws, score=sc, stream=stream)
+                else:
+                    self.recompute_layer(n, cu_rows, cu_keys, x[rows], m["row_pos"][rows], m["write_slots"][rows],
+                                         read[b0 * nk:b1 * nk], score=sc, stream=stream)
         if layer_hook is not None:
             layer_hook(n_run, x)
         return x
@@ -211,16 +250,25 @@ class AffixBatch:
         read_slots [n_keys] (the donor's logical view)."""
         n = donor_x.shape[0]
         for i in range(self.model.n_layers):
-            A.acache_layer_recompute(self.model.dims, self.model.lw[i], [0, n], [0, read_slots.numel()], donor_x,
-                                     donor_pos, write_slots, read_slots, self.k_pools[i], self.v_pools[i], self.ws,
-                                     stream=stream)
+            self.recompute_layer(i, [0, n], [0, read_slots.numel()], donor_x, donor_pos, write_slots, read_slots,
+                                 stream=stream)
         return donor_x
 
     def shift_affix(self, delta: int, stream=None):
         """Reuse the shared affix cache delta positions from where it was
-        materialised: its K rows are re-rotated in place at every layer."""
+        materialised: its K rows are re-rotated in place at every layer (8-bit
+        caches: read back, turned and stored again)."""
         slots = self.affix_slots
-        d = torch.full((self.L,), int(delta), dtype=torch.int32, device=self.device)
+        with _on(stream):
+            d = torch.full((self.L,), int(delta), dtype=torch.int32, device=self.device)
+            rows = torch.arange(self.L, dtype=torch.int32, device=self.device)
+        for c in self.caches:
+            with _on(stream):
+                k, v = (torch.empty((self.L, self.model.kv_width), dtype=self.model.dtype, device=self.device)
+                        for _ in range(2))
+            A.acache_quant_load(self.model.dims, c, slots, k, v, stream=stream)
+            A.acache_rerotate_k(self.model.dims, k, rows, k, rows, d, stream=stream)
+            A.acache_quant_store(self.model.dims, c, k, v, slots, ws=self.ws, stream=stream)
         for k in self.k_pools:
             A.acache_rerotate_k(self.model.dims, k, slots, k, slots, d, stream=stream)
 
@@ -267,7 +315,10 @@ class AffixBatch:
         a full-prompt forward of every request through the selection layer
         (the first whose affix K/V depend on context), then each affix
         token's squared K/V deviation from the shared cache, then Eq. 6's
-        top-K.  Returns (anchors [B, k], scores [B, L])."""
+        top-K.  Returns (anchors [B, k], scores [B, L]).  Not over 8-bit caches
+        (their entries' rounding is no deviation)."""
+        if self.quant_block:
+            raise ValueError("the KV-deviation selector reads bf16 or fp32 pools")
         n = min(1, self.model.n_layers - 1)
         every = torch.arange(self.L, dtype=torch.int32, device=self.device).repeat(self.B, 1).contiguous()
         m = self.maps(every, self.L, stream)
@@ -412,13 +463,13 @@ def decode_step(batch: AffixBatch, plan: DecodePlan, blk: int, m: dict, anchors:
     whole logical context, the view the refresh (maps ``m``, anchor set
     ``anchors``) left.  With split_shared (bf16) the view is read as the
     shared affix minus the anchors, taken for all requests together, plus
-    each request's private slots (acache_layer_decode); otherwise through
-    the read-slot map.  Returns the block's last-layer rows [B * block_len, d]."""
+    each request's private slots (acache_layer_decode); otherwise, and over
+    8-bit caches, through the read-slot map.  Returns the block's last-layer rows [B * block_len, d]."""
     B, blen = batch.B, plan.block_len
     h = A.acache_gather_rows(batch.x_src, plan.pos[blk], batch.remap, stream=stream)
     wslots = plan.write_slots(batch, blk)
     k = plan.k
-    if split_shared and batch.model.dims.dtype == A.ACACHE_BF16:
+    if split_shared and batch.model.dims.dtype == A.ACACHE_BF16 and not batch.quant_block:
         R = batch.rows_per_request(k)
         anc = plan.anchors if plan.full else anchors
         if anc is None and k > 0:
@@ -431,9 +482,7 @@ def decode_step(batch: AffixBatch, plan: DecodePlan, blk: int, m: dict, anchors:
     cu_rows = [b * blen for b in range(B + 1)]
     cu_keys = [b * batch.S for b in range(B + 1)]
     for i in range(batch.model.n_layers):
-        A.acache_layer_recompute(batch.model.dims, batch.model.lw[i], cu_rows, cu_keys, h, plan.row_pos[blk],
-                                 wslots, m["read_slots"], batch.k_pools[i], batch.v_pools[i], batch.ws,
-                                 stream=stream)
+        batch.recompute_layer(i, cu_rows, cu_keys, h, plan.row_pos[blk], wslots, m["read_slots"], stream=stream)
     return h
 
 

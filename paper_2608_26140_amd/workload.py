@@ -49,7 +49,8 @@ class Setup:
 
 
 def build(w: W.Workload, device="cuda", n_layers: Optional[int] = None, keep_host: bool = True,
-          max_rows: Optional[int] = None, block_size: Optional[int] = None) -> Setup:
+          max_rows: Optional[int] = None, block_size: Optional[int] = None,
+          quant_block: Optional[int] = None) -> Setup:
     d, lay = w.dims, w.layout
     nl = d.n_layers if n_layers is None else n_layers
     host = {"layers": []}
@@ -76,7 +77,7 @@ def build(w: W.Workload, device="cuda", n_layers: Optional[int] = None, keep_hos
         x_src = upload(hidden.reshape(B * S, d.d_model), d.dtype, device)
         remap = None
     batch = AffixBatch(model, S, lay.affix_begin, lay.affix_len, lay.mask_begin, lay.mask_len, B, x_src,
-                       remap, device=device, max_rows=max_rows, block_size=block_size)
+                       remap, device=device, max_rows=max_rows, block_size=block_size, quant_block=quant_block)
 
     L = lay.affix_len
     if w.stale == "perturb":

@@ -174,3 +174,40 @@ def test_clear_takes_whole_blocks(A):
     assert p.v_scales[:, 1].tolist() == [1, 0, 0, 1, 1, 1, 0]
     p.clear()
     assert not p.k_scales.any() and not p.v_scales.any()
+
+
+def test_layer_refusals(A):
+    lib, dims, p = A.lib, A.make_dims(*DIMS), ctypes.c_void_p(16)
+    w = A.LayerWeights(16, 16, 16, 16, 16, 16)
+
+    def call(dims=dims, rows=(0, 3), keys=(0, 5), x=p, pos=p, wsl=p, rsl=p, desc=None, ws=p, wsb=1 << 40, score=None):
+        rg, keep = A._ragged(rows, keys)
+        return lib.acache_quant_layer_recompute(
+            ctypes.byref(dims), ctypes.byref(w), ctypes.byref(rg), x, pos, wsl, rsl, ctypes.byref(desc or pool(A)),
+            ctypes.byref(score) if score else None, ws, wsb, None)
+    assert call(dims=A.make_dims(256, 4, 4, 64, 688, "f32")) == 4
+    assert call(rows=(0, 0)) == 0
+    assert call(keys=(0, 0)) == 2
+    assert call(x=None) == 1 and call(pos=None) == 1 and call(wsl=None) == 1 and call(rsl=None) == 1
+    assert call(desc=pool(A, n_slots=0)) == 2
+    assert call(desc=pool(A, n_slots=1 << 20)) == 4
+    assert call(desc=pool(A, v_scales=None)) == 1 and call(desc=pool(A, block=24)) == 4
+    assert call(x=ctypes.c_void_p(8)) == 3
+    assert call(ws=None) == 5 and call(wsb=1000) == 5
+    cq = (ctypes.c_int32 * 2)(0, 4)
+    assert call(score=A.ScoreArgs(16, cq, 16, 10, 0, 16)) == 2      # more masked rows than rows
+    cq2 = (ctypes.c_int32 * 2)(0, 2)
+    assert call(score=A.ScoreArgs(16, cq2, 16, 10, 9, 16)) == 4     # unknown normalisation
+    assert call(score=A.ScoreArgs(None, cq2, 16, 10, 0, 16)) == 1
+
+
+def test_layer_workspace_size(A):
+    lib, dims = A.lib, A.make_dims(*DIMS)
+
+    def size(rows, batch=1, L=0, **kw):
+        return lib.acache_quant_layer_workspace_size(ctypes.byref(dims), rows, batch, L, ctypes.byref(pool(A, **kw)))
+    assert size(32) > lib.acache_workspace_size(ctypes.byref(dims), 32, 1, 0)
+    assert size(700, 2, 512) >= size(700, 2, 100) >= size(700, 1, 100) >= size(600, 1, 100) > 0
+    assert size(-1) == 0 and size(1, block=5) == 0
+    f32 = A.make_dims(256, 4, 4, 64, 688, "f32")
+    assert lib.acache_quant_layer_workspace_size(ctypes.byref(f32), 1, 1, 0, ctypes.byref(pool(A))) == 0
