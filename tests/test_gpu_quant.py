@@ -406,6 +406,92 @@ def test_attention_near_the_offset_limit():
     assert np.abs(k64).max() > 1  # the rows arrived
 
 
+# Many queries: the 256-query kernel (whole tiles, one of 64 requests each a
+# workgroup a head; few keys up), with key splits, and with the 32-query kernel
+# on what is left of the requests.
+MANY = [
+    ("one key", 4, 4, [256] * 64, [1] * 64),
+    ("two tiles of keys and fewer", 4, 4, [256 - b % 5 * 7 for b in range(64)], [33 + b for b in range(64)]),
+    ("ragged", 4, 4, [256 - b % 5 * 7 for b in range(64)], [500 - 3 * b for b in range(64)]),
+    ("grouped heads", 28, 4, [36] * 64, [300 + b for b in range(64)]),
+    ("some without rows", 4, 2, [0 if b % 9 == 4 else 500 for b in range(64)], [901 - b for b in range(64)]),
+    ("key splits", 28, 4, [256, 200], [5120, 4999]),
+    ("more key splits", 16, 4, [256, 300], [5000, 5063]),
+    ("with remainders", 4, 4, [286 - b % 7 for b in range(64)], [600 - b for b in range(64)]),
+    ("grouped, with remainders", 8, 1, [130] * 64, [900 - b for b in range(64)]),
+    ("long and short remainders", 32, 32, [794 - 11 * b for b in range(8)], [2432 - 17 * b for b in range(8)]),
+]
+
+
+def sampled(cu_rows, per, rng):
+    """A few rows of each request, its first and last among them."""
+    return [np.unique(np.r_[a, b - 1, rng.integers(a, b, per)]) if b > a else np.zeros(0, dtype=int)
+            for a, b in zip(cu_rows[:-1], cu_rows[1:])]
+
+
+def check_many(p, rows, keys, slots, q, out, lse, what):
+    cu_rows, cu_keys = (np.concatenate([[0], np.cumsum(n)]).astype(int) for n in (rows, keys))
+    rows_of_req = sampled(cu_rows, 3, p.rng)
+    at = torch.from_numpy(np.concatenate(rows_of_req)).to(DEV)
+    cu = np.concatenate([[0], np.cumsum([len(r) for r in rows_of_req])]).astype(int).tolist()
+    check_attention(p, q[at], cu, cu_keys.tolist(), slots, out[at], lse[at], what)
+
+
+def many(p, rows, keys, slots, q=None, ws=True, what=""):
+    n, H = int(np.sum(rows)), p.dims.n_heads
+    cu_rows, cu_keys = (np.concatenate([[0], np.cumsum(x)]).astype(int).tolist() for x in (rows, keys))
+    if q is None:
+        q = (1.3 * torch.randn(n, H * 128, device=DEV, generator=torch.Generator(DEV).manual_seed(n))).to(torch.bfloat16)
+    out = torch.full((n + 1, H * 128), float("nan"), dtype=torch.bfloat16, device=DEV)
+    lse = torch.full((n + 1, H), float("nan"), device=DEV)
+    w = None
+    if ws:
+        w = A.quant_workspace(p.dims, n, p.pool)
+        w.fill_(0xFF)
+    A.acache_quant_attention(p.dims, cu_rows, cu_keys, q, up_i32(slots), p.pool, out=out, lse=lse, ws=w)
+    torch.cuda.synchronize()
+    assert torch.isnan(out[n]).all() and torch.isnan(lse[n]).all()
+    assert torch.isfinite(out[:n].float()).all() and torch.isfinite(lse[:n]).all()
+    check_many(p, rows, keys, slots, q, out[:n], lse[:n], what)
+    return out[:n], lse[:n]
+
+
+@pytest.mark.parametrize("what,H,Hkv,rows,keys", MANY, ids=[m[0] for m in MANY])
+def test_attention_many_queries(what, H, Hkv, rows, keys):
+    p = filled(H, Hkv, 1900, 64, seed=len(what))
+    p.pool.clear(slice(640, 768))  # two empty blocks
+    for r in p.ref:
+        r.scales[10:12] = 0.0
+    slots = p.rng.integers(-40, 1940, int(np.sum(keys)))
+    out, lse = many(p, rows, keys, slots, what=what)
+    again, lse2 = many(p, rows, keys, slots, what=what + ", again")
+    assert torch.equal(out, again) and torch.equal(lse, lse2)  # the same bits every time
+    many(p, rows, keys, slots, ws=False, what=what + ", no workspace")
+
+
+def test_attention_many_queries_values():
+    """Logits of some hundreds, maxima that move late, NaN in one key."""
+    p = filled(4, 4, 1000, 64, seed=31)
+    rows, keys = [256] * 64, [300] * 64
+    big = np.zeros((1, 4, 128)) + 40.0
+    p.store([999], x=[big, big], check=False)
+    slots = p.rng.integers(0, 999, 64 * 300).reshape(64, 300)
+    slots[::2, -1] = 999
+    slots[1::2, 0] = 999
+    g = torch.Generator(DEV).manual_seed(5)
+    q = (20 * torch.randn(64 * 256, 512, device=DEV, generator=g)).to(torch.bfloat16)
+    many(p, rows, keys, slots.reshape(-1), q=q, what="large")
+    x = p.rng.normal(0, 1, (1, 4, 128))
+    x[0, 2, 3] = np.nan
+    p.store([998], x=[x, np.nan_to_num(x)], check=False)
+    slots[:, 150] = 997
+    slots[slots == 998] = 996
+    slots[5, 150] = 998
+    out = A.acache_quant_attention(p.dims, np.arange(65) * 256, np.arange(65) * 300, q, up_i32(slots.reshape(-1)), p.pool)
+    bad = torch.isnan(out.view(64, 256, 4, 128)).any(-1)
+    assert bad[5, :, 2].all() and int(bad.sum()) == 256
+
+
 # ---------------------------------------------------------------------------- together
 def test_store_attend_load_together_and_captured():
     """A decode loop's calls: rows of a block overwrite their slots, the view
