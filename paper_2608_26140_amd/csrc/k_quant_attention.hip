@@ -36,9 +36,9 @@ typedef short v4i16 __attribute__((__vector_size__(4 * sizeof(short))));
 
 constexpr int kDh = 128;
 constexpr int kTileK = 64;             // keys per tile
-constexpr int kCodeTileB = kTileK * kDh;      // 8 KB: the codes of one K or V tile
 constexpr int kRowB = kDh * 2;                // a converted row
 constexpr int kTileB = kTileK * kRowB;        // 16 KB: a converted tile
+constexpr int kAuxB = kTileK * 4;             // a 32-bit value for each key of a tile
 constexpr int kMaxSplits = 64;
 // buffer offset of an absent key: past every pool the entry point admits, so
 // its copies give zeros
@@ -148,33 +148,28 @@ __device__ __forceinline__ void write_query(const QAttnArgs& a, int64_t pair, in
 
 // ============================================================================
 // quant_attention_wide_kernel: 256 queries of one KV head and request a
-// workgroup, 8 waves of 32.  Every wave reads the same 64-key tiles: the codes
-// of K and V come to LDS by buffer copies some tiles ahead (issued from inline
-// assembly, which the compiler's wait analysis does not drain, and waited for
-// by counting), the slots and scales that the copies' addresses need earlier
-// still, by waves 0, 1 and 2.  Each wave converts the rows it copied to bf16
-// one iteration ahead of their use: eight conversions of K and of V for a
-// lane's 32 logits.
+// workgroup, 8 waves of 32, one workgroup a CU.  Every wave reads the same
+// 64-key tiles of K and V in LDS, as bf16, four of each.  A wave takes its rows
+// of a tile's codes into registers at the start of an iteration and converts
+// them behind its products, so that K and V are converted once for all the
+// queries: eight conversions of each for a lane's 32 logits.  (Codes copied to
+// LDS first, three tiles ahead, with slots and scales in rings of their own:
+// 286 us where this takes 270, 6052 rows of 32 heads over 2432 keys.)
 // The loop is software pipelined: iteration t forms S(t + 1) while it
 // exponentiates tile t's logits, then adds tile t's P V while it takes tile
-// t + 1's maxima, and converts K(t + 2) and V(t + 1).
+// t + 1's maxima, and converts K(t + 3) and V(t + 2); a barrier at every second
+// iteration orders that (at every one, with two tiles: 276).
+// With 64-query waves or 128-query workgroups, two a CU, the registers do not
+// suffice.  What remains between the loop and the matrix units' rate is spread
+// over its parts: 182 us of products alone, 30 of exponentials, 23 and 17 of
+// K and V fragment reads, 20 of conversions.
 // ============================================================================
-constexpr int kWdWaves = 8;
-constexpr int kWdThreads = 64 * kWdWaves;
-constexpr int kWdTileQ = 32 * kWdWaves;
-constexpr int kWdStages = 4;  // rings of K and V codes
-constexpr int kWdAux = 8;     // rings of slots and scales
-constexpr int kAuxB = kTileK * 4;
-constexpr int kWdKAhead = 3, kWdVAhead = 2;  // fragments read ahead of their product
+constexpr int kWdWaves = 8, kWdThreads = 64 * kWdWaves, kWdTileQ = 32 * kWdWaves;
+constexpr int kWdKAhead = 4, kWdVAhead = 3;  // fragments read ahead of their product
 
 __global__ __launch_bounds__(kWdThreads, 1) void quant_attention_wide_kernel(QAttnArgs a) {
-  __shared__ __attribute__((aligned(1024))) char k_codes[kWdStages * kCodeTileB];
-  __shared__ __attribute__((aligned(1024))) char v_codes[kWdStages * kCodeTileB];
-  __shared__ __attribute__((aligned(1024))) char k_tile[2 * kTileB];
-  __shared__ __attribute__((aligned(1024))) char v_tile[2 * kTileB];
-  __shared__ __attribute__((aligned(256))) char slot_ring[kWdAux * kAuxB];
-  __shared__ __attribute__((aligned(256))) char ks_ring[kWdAux * kAuxB];
-  __shared__ __attribute__((aligned(256))) char vs_ring[kWdAux * kAuxB];
+  __shared__ __attribute__((aligned(1024))) char k_tile[4 * kTileB];
+  __shared__ __attribute__((aligned(1024))) char v_tile[4 * kTileB];
 
   const Unit un = unit_of(a.rg, a.splits, (a.p.heads & 7) == 0 ? a.p.heads >> 3 : 1);
   const int g = un.g, b = un.b;
@@ -198,51 +193,40 @@ __global__ __launch_bounds__(kWdThreads, 1) void quant_attention_wide_kernel(QAt
   const uint32_t n_slots = (uint32_t)a.p.n_slots;
   const uint32_t pool_b = (uint32_t)(a.p.n_slots * a.p.ld);  // < 2^31
   const uint32_t scale_b = (uint32_t)(((a.p.n_slots + (1 << a.p.shift) - 1) >> a.p.shift) * a.p.heads * 4);
-  const rsrc_words kres = buffer_words(a.p.codes[0], pool_b), vres = buffer_words(a.p.codes[1], pool_b);
-  const rsrc_words ksres = buffer_words(a.p.scales[0], scale_b), vsres = buffer_words(a.p.scales[1], scale_b);
-  const rsrc_words sres = buffer_words(a.slots + a.rg.cu_keys[b], (uint32_t)S * 4u);
+  const auto kres = buffer_rsrc(a.p.codes[0], pool_b), vres = buffer_rsrc(a.p.codes[1], pool_b);
+  const auto ksres = buffer_rsrc(a.p.scales[0], scale_b), vsres = buffer_rsrc(a.p.scales[1], scale_b);
+  const auto sres = buffer_rsrc(a.slots + a.rg.cu_keys[b], (uint32_t)S * 4u);
   const uint32_t ld = (uint32_t)a.p.ld;
 
-  auto aux = [](char* ring, int t) { return ring + (t & (kWdAux - 1)) * kAuxB; };
-  // tiles are counted from the first one
-  auto issue_slots = [&](int t) { dma4_asm(sres, (uint32_t)(key0 + t * kTileK + lane) * 4u, aux(slot_ring, t)); };
-  // whether key i of tile t is there, and its slot
-  auto has_key = [&](int t, int i, int& slot) {
-    slot = *reinterpret_cast<const int*>(aux(slot_ring, t) + i * 4);
-    return t * kTileK + i < n_keys && (uint32_t)slot < n_slots;
-  };
-  // the scales of tile t's keys
-  auto issue_scales = [&](int t, rsrc_words res, char* ring) {
-    int slot;
-    const bool ok = has_key(t, lane, slot);
-    dma4_asm(res, ok ? (uint32_t)((slot >> a.p.shift) * a.p.heads + g) * 4u : kAbsent, aux(ring, t));
-  };
-  auto issue_aux = [&](int t_slots) {
-    if (wave == 0) issue_slots(t_slots);
-    if (wave == 1) issue_scales(t_slots - 1, ksres, ks_ring);
-    if (wave == 2) issue_scales(t_slots - 1, vsres, vs_ring);
-  };
   // This wave's rows of a tile, one 16-byte chunk of codes a lane: row kk.
+  // Tiles are counted from the first one.
   const int kk = wave * 8 + (lane >> 3), ch = lane & 7;
-  auto issue_codes = [&](int t, rsrc_words res, char* ring) {
-    int slot;
-    const bool ok = has_key(t, kk, slot);
-    const uint32_t off = (uint32_t)slot * ld + (uint32_t)g * kDh + ch * 16;
-    dma16_asm(res, ok ? off : kAbsent, ring + (t & (kWdStages - 1)) * kCodeTileB + wave * 1024);
-  };
-  // Converted rows have 16-byte chunk c of row r at c ^ (r & 15) (K) and at
-  // c ^ (4 (r & 3) ^ (r & 1)) (V): sixteen lanes' fragment reads and writes of
-  // K, and 32 lanes' transposing reads of V (four rows of four chunks), then
-  // cover all the banks.
   struct Row {
     u32x4 codes;
     float scale;
   };
-  auto read_row = [&](int t, const char* ring, char* scales) {
-    return Row{*reinterpret_cast<const u32x4*>(ring + (t & (kWdStages - 1)) * kCodeTileB + wave * 1024 + lane * 16),
-               *reinterpret_cast<const float*>(aux(scales, t) + kk * 4)};
+  struct Where {  // byte offsets of the row's codes and scale
+    uint32_t code, scale;
   };
-  auto convert = [&](int t, Row r, char* tile, int swizzle) {
+  auto load_slot = [&](int t) {
+    return (int)__builtin_amdgcn_raw_buffer_load_b32(sres, (uint32_t)(key0 + t * kTileK + kk) * 4u, 0, 0);
+  };
+  auto locate = [&](int t, int slot) {
+    const bool ok = t * kTileK + kk < n_keys && (uint32_t)slot < n_slots;
+    return Where{ok ? (uint32_t)slot * ld + (uint32_t)g * kDh + ch * 16 : kAbsent,
+                 ok ? (uint32_t)((slot >> a.p.shift) * a.p.heads + g) * 4u : kAbsent};
+  };
+  auto load_row = [](Where x, __amdgpu_buffer_rsrc_t codes, __amdgpu_buffer_rsrc_t scales) {
+    return Row{__builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(codes, x.code, 0, 0)),
+               __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(scales, x.scale, 0, 0))};
+  };
+  auto load_k = [&](Where x) { return load_row(x, kres, ksres); };
+  auto load_v = [&](Where x) { return load_row(x, vres, vsres); };
+  // Converted rows have 16-byte chunk c of row r at c ^ (r & 15) (K) and at
+  // c ^ (4 (r & 3) ^ (r & 1)) (V): sixteen lanes' fragment reads and writes of
+  // K, and 32 lanes' transposing reads of V (four rows of four chunks), then
+  // cover all the banks.
+  auto convert = [&](Row r, char* tile, int swizzle) {
     // an empty block's codes stand for zeros
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(r.scale > 0.f)) != 0, 0)) {
 #pragma unroll
@@ -250,14 +234,12 @@ __global__ __launch_bounds__(kWdThreads, 1) void quant_attention_wide_kernel(QAt
     }
     u32x4 c[2];
     convert16(r.codes, r.scale, c);
-    char* row = tile + (t & 1) * kTileB + kk * kRowB;
+    char* row = tile + kk * kRowB;
     *reinterpret_cast<u32x4*>(row + (((2 * ch) ^ swizzle) << 4)) = c[0];
     *reinterpret_cast<u32x4*>(row + (((2 * ch + 1) ^ swizzle) << 4)) = c[1];
   };
-  auto read_k = [&](int t) { return read_row(t, k_codes, ks_ring); };
-  auto read_v = [&](int t) { return read_row(t, v_codes, vs_ring); };
-  auto convert_k = [&](int t, const Row& r) { convert(t, r, k_tile, kk & 15); };
-  auto convert_v = [&](int t, const Row& r) { convert(t, r, v_tile, ((kk & 3) << 2) ^ (kk & 1)); };
+  auto convert_k = [&](int t, const Row& r) { convert(r, k_tile + (t & 3) * kTileB, kk & 15); };
+  auto convert_v = [&](int t, const Row& r) { convert(r, v_tile + (t & 3) * kTileB, ((kk & 3) << 2) ^ (kk & 1)); };
 
   const float scale = kLog2e * rsqrtf((float)kDh);
   const int krow = key_perm(lane & 31);
@@ -268,12 +250,12 @@ __global__ __launch_bounds__(kWdThreads, 1) void quant_attention_wide_kernel(QAt
   const int v_byte = (gi & 1) * 8, v_sw = (gi & 12) ^ ((gi >> 2) & 1);
   auto kfrag = [&](int t, int i) {
     const int kb = i >> 3, s = i & 7;
-    return *reinterpret_cast<const bf16x8*>(k_tile + (t & 1) * kTileB + kb * 32 * kRowB + k_off +
+    return *reinterpret_cast<const bf16x8*>(k_tile + (t & 3) * kTileB + kb * 32 * kRowB + k_off +
                                             (((2 * s + hl) ^ k_sw) << 4));
   };
   auto vfrag = [&](int t, int i) {
     const int kb = i >> 3, g2 = (i >> 2) & 1, d = i & 3;
-    const char* row = v_tile + (t & 1) * kTileB + (kb * 32 + g2 * 16 + v_key) * kRowB;
+    const char* row = v_tile + (t & 3) * kTileB + (kb * 32 + g2 * 16 + v_key) * kRowB;
     const int off = ((4 * d + v_chunk) ^ v_sw) * 16 + v_byte;
     const v4i16 lo = ds_read_tr16(row + off);
     const v4i16 hi = ds_read_tr16(row + 4 * kRowB + off);
@@ -319,27 +301,19 @@ __global__ __launch_bounds__(kWdThreads, 1) void quant_attention_wide_kernel(QAt
     return fmaxf(mx, __shfl_xor(mx, 32)) * scale;
   };
 
+  int slot = 0;         // of tile t + 3 at iteration t
+  Where v_at = {0, 0};  // of tile t + 2
   if (n_t > 0) {
-    // prologue: the slots of six tiles, the scales of five, the codes of four
-    // K tiles and three V tiles
-    if (wave == 0)
-      for (int i = 0; i < 6; ++i) issue_slots(i);
-    wait_vm_asm<0>();
-    bare_barrier();
-    if (wave == 1)
-      for (int i = 0; i < 5; ++i) issue_scales(i, ksres, ks_ring);
-    if (wave == 2)
-      for (int i = 0; i < 5; ++i) issue_scales(i, vsres, vs_ring);
-    issue_codes(0, kres, k_codes);
-    for (int i = 0; i < 3; ++i) {
-      issue_codes(i + 1, kres, k_codes);
-      issue_codes(i, vres, v_codes);
-    }
-    wait_vm_asm<4>();  // the scales; K of two tiles, V of one
-    bare_barrier();
-    convert_k(0, read_k(0));
-    convert_k(1, read_k(1));
-    convert_v(0, read_v(0));
+    const int s0 = load_slot(0), s1 = load_slot(1), s2 = load_slot(2);
+    slot = load_slot(3);
+    const Where x0 = locate(0, s0), x1 = locate(1, s1);
+    v_at = locate(2, s2);
+    const Row k0 = load_k(x0), v0 = load_v(x0), k1 = load_k(x1), v1 = load_v(x1), k2 = load_k(v_at);
+    convert_k(0, k0);
+    convert_v(0, v0);
+    convert_k(1, k1);
+    convert_v(1, v1);
+    convert_k(2, k2);
     wait_lgkmcnt<0>();
     bare_barrier();
     if (live) {
@@ -353,76 +327,84 @@ __global__ __launch_bounds__(kWdThreads, 1) void quant_attention_wide_kernel(QAt
       rescale(tile_max(0, st_a));
     }
   }
-  auto step = [&](int t, f32x16 (&cur)[2], f32x16 (&nxt)[2]) {
-    // all but the last iteration's two copies of codes have landed: K codes up
-    // to t + 2, V codes to t + 1, scales to t + 4, slots to t + 5; and what
-    // this wave converted is written
-    wait_vm_asm<2>();
-    wait_lgkmcnt<0>();
-    bare_barrier();
-    issue_aux(t + 6);
+  auto step = [&](int t, f32x16 (&cur)[2], f32x16 (&nxt)[2], bool sync) {
+    // K to tile t + 2 and V to tile t + 1 are written, and what iterations t
+    // and t + 1 write over has been read, by every wave
+    if (sync) {
+      wait_lgkmcnt<0>();
+      bare_barrier();
+    }
+    __builtin_amdgcn_s_setprio(1);  // ahead of a wave that is between iterations
+    const Where k_at = locate(t + 3, slot);
+    const Row row_k = load_k(k_at), row_v = load_v(v_at);
+    v_at = k_at;
+    slot = load_slot(t + 4);
     if (!live) {
-      issue_codes(t + 4, kres, k_codes);
-      issue_codes(t + 3, vres, v_codes);
-      convert_k(t + 2, read_k(t + 2));
-      convert_v(t + 1, read_v(t + 1));
+      __builtin_amdgcn_s_setprio(0);
+      convert_k(t + 3, row_k);
+      convert_v(t + 2, row_v);
       return;
     }
     const float m_use = m_run == -INFINITY ? 0.f : m_run;
     float psum = 0.f, mx = -INFINITY;
     bf16x8 pb[2][2];
     bf16x8 kf[kWdKAhead + 1], vf[kWdVAhead + 1];
+    auto weight = [&](int e) {
+      const int kb = e >> 4, r = e & 15;
+      const float x = __builtin_amdgcn_exp2f(fmaf(cur[kb][r], scale, -m_use));
+      psum += x;
+      pb[kb][r >> 3][r & 7] = (bf16)x;
+    };
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int r = 0; r < 16; ++r) nxt[kb][r] = 0.f;
 #pragma unroll
     for (int i = 0; i < kWdKAhead; ++i) kf[i] = kfrag(t + 1, i);
-    // sixteen products of S(t + 1), each with two of tile t's exponentials,
-    // then sixteen of P V, each with the maxima of two of tile t + 1's logits.
-    // The empty asm statements keep the running sum and maximum in their place.
+    // sixteen products of S(t + 1), each with an exponential of tile t, then
+    // sixteen of P V: the first eight with two exponentials each, the others
+    // with the maxima of four of tile t + 1's logits.  The empty asm statements
+    // keep the running sum and maximum in their place.
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      if (i == 1) issue_codes(t + 4, kres, k_codes);
-      if (i == 3) issue_codes(t + 3, vres, v_codes);
       if (i + kWdKAhead < 16) kf[(i + kWdKAhead) % (kWdKAhead + 1)] = kfrag(t + 1, i + kWdKAhead);
       if (i >= 16 - kWdVAhead) vf[i - (16 - kWdVAhead)] = vfrag(t, i - (16 - kWdVAhead));
       nxt[i >> 3] = mfma32x32x16(kf[i % (kWdKAhead + 1)], qf[i & 7], nxt[i >> 3]);
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int e = 2 * i + u, kb = e >> 4, r = e & 15;
-        const float x = __builtin_amdgcn_exp2f(fmaf(cur[kb][r], scale, -m_use));
-        psum += x;
-        pb[kb][r >> 3][r & 7] = (bf16)x;
-      }
+      weight(i);
       asm volatile("" ::"v"(psum));
       __builtin_amdgcn_sched_barrier(0);
     }
-    l_part += psum;
-    Row row_k, row_v;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       if (i + kWdVAhead < 16) vf[(i + kWdVAhead) % (kWdVAhead + 1)] = vfrag(t, i + kWdVAhead);
       o_acc[i & 3] = mfma32x32x16(vf[i % (kWdVAhead + 1)], pb[i >> 3][(i >> 2) & 1], o_acc[i & 3]);
-      mx = fmaxf(mx, fmaxf(nxt[i >> 3][2 * (i & 7)], nxt[i >> 3][2 * (i & 7) + 1]));
-      asm volatile("" ::"v"(mx));
-      if (i == 0) row_k = read_k(t + 2);
-      if (i == 2) row_v = read_v(t + 1);
-      if (i == 5) convert_k(t + 2, row_k);
-      if (i == 9) convert_v(t + 1, row_v);
+      if (i < 8) {
+        weight(16 + 2 * i);
+        weight(17 + 2 * i);
+        asm volatile("" ::"v"(psum));
+      } else {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) mx = fmaxf(mx, nxt[(i - 8) >> 2][4 * (i & 3) + u]);
+        asm volatile("" ::"v"(mx));
+      }
+      if (i == 10) convert_k(t + 3, row_k);
+      if (i == 13) convert_v(t + 2, row_v);
       __builtin_amdgcn_sched_barrier(0);
     }
+    l_part += psum;
+    __builtin_amdgcn_s_setprio(0);
     if (t + 1 < n_t) {
       if ((t + 2) * kTileK > n_keys) mx = tile_max(t + 1, nxt);
       else mx = fmaxf(mx, __shfl_xor(mx, 32)) * scale;
       rescale(mx);
     }
   };
-  for (int t = 0; t < n_t; t += 2) {
-    step(t, st_a, st_b);
-    if (t + 1 < n_t) step(t + 1, st_b, st_a);
+  for (int t = 0; t < n_t; t += 4) {
+    step(t, st_a, st_b, true);
+    if (t + 1 < n_t) step(t + 1, st_b, st_a, false);
+    if (t + 2 < n_t) step(t + 2, st_a, st_b, true);
+    if (t + 3 < n_t) step(t + 3, st_b, st_a, false);
   }
-  wait_vm_asm<0>();  // every copy has landed before the workgroup's LDS is given away
 
   if (!live) return;
   const float l_tot = l_part + __shfl_xor(l_part, 32);
