@@ -1007,6 +1007,7 @@ acache_status acache_quant_attention(const acache_dims* dims, const acache_ragge
   st = check_quant_buffers(p);
   if (st != ACACHE_OK) return st;
   CHECK(p.n_slots * p.ld < ((int64_t)1 << 31), ACACHE_ERR_UNSUPPORTED);  // 32-bit offsets
+  CHECK((int64_t)r.cu_rows[r.batch] * dims->n_heads < ((int64_t)1 << 31), ACACHE_ERR_UNSUPPORTED);
   CHECK(aligned16(q) && aligned16(out), ACACHE_ERR_ALIGN);
   CHECK(!ws || aligned16(ws), ACACHE_ERR_ALIGN);
   LAUNCH_T(ACACHE_K_ATTENTION, stream,

@@ -644,80 +644,79 @@ __global__ __launch_bounds__(64 * kNwWaves, 2) void quant_attention_narrow_kerne
 
   // the waves' results, lane by lane: 1 into 0 and 3 into 2, then 2 into 0
   float l = l_part + __shfl_xor(l_part, 32), m = m_run;
-  float* const res = reinterpret_cast<float*>(lds);
 #pragma unroll
   for (int round = 0; round < 2; ++round) {
     const bool give = round == 0 ? (wave & 1) : wave == 2, take = round == 0 ? !(wave & 1) : wave == 0;
-    float* const at = res + (round == 0 ? wave >> 1 : 0) * (66 * 64);
+    f32x4* const o_at = reinterpret_cast<f32x4*>(lds + (round == 0 ? wave >> 1 : 0) * (66 * 64 * 4)) + lane;
+    float2* const ml_at = reinterpret_cast<float2*>(o_at - lane + 16 * 64) + lane;
     __syncthreads();
     if (give) {
 #pragma unroll
-      for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) at[(16 * d + r) * 64 + lane] = o_acc[d][r];
-      at[64 * 64 + lane] = m;
-      at[65 * 64 + lane] = l;
+      for (int i = 0; i < 16; ++i)
+        o_at[i * 64] = f32x4{o_acc[i >> 2][4 * (i & 3)], o_acc[i >> 2][4 * (i & 3) + 1], o_acc[i >> 2][4 * (i & 3) + 2],
+                             o_acc[i >> 2][4 * (i & 3) + 3]};
+      *ml_at = float2{m, l};
     }
     __syncthreads();
     if (take) {
-      const float m2 = at[64 * 64 + lane], l2 = at[65 * 64 + lane];
-      const float mn = fmaxf(m, m2);
+      const float2 ml = *ml_at;
+      const float mn = fmaxf(m, ml.x);
       const float f0 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-      const float f1 = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m2 - mn);
-      l = l * f0 + l2 * f1;
+      const float f1 = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - mn);
+      l = l * f0 + ml.y * f1;
       m = mn;
 #pragma unroll
-      for (int d = 0; d < 4; ++d)
+      for (int i = 0; i < 16; ++i) {
+        const f32x4 o = o_at[i * 64];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o_acc[d][r] = o_acc[d][r] * f0 + at[(16 * d + r) * 64 + lane] * f1;
+        for (int j = 0; j < 4; ++j)
+          o_acc[i >> 2][4 * (i & 3) + j] = o_acc[i >> 2][4 * (i & 3) + j] * f0 + o[j] * f1;
+      }
     }
   }
   if (wave == 0 && q_ok) write_query(a, pair, un.split, hl, o_acc, m, l);
 }
 
 // Combines the key splits of each (row, head): m = max_s m_s, O = sum_s
-// 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s, the sums in split order.  32 lanes
-// per (row, head): lane s holds splits s and 32 + s's max and sum, and each
-// lane sums 4 dimensions, the O_s of four splits in flight at a time.
+// 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  A wave per (row, head): lane s holds
+// split s's max and sum; lane half hf sums 4 dimensions a lane over the splits
+// s with (s / 8) % 2 == hf, in order, eight loads in flight at a time (a chain
+// of loads is what bounds it), and the halves are added last.
 __global__ __launch_bounds__(256) void quant_attention_merge_kernel(const float* __restrict__ part_o,
                                                                     const float* __restrict__ part_ml, int splits,
                                                                     int64_t pairs, bf16* __restrict__ out,
                                                                     float* __restrict__ lse) {
-  const int64_t pair = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int64_t pair = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (pair >= pairs) return;
-  const int lane = threadIdx.x & 31;
-  float2 ml[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    ml[i] = float2{-INFINITY, 0.f};
-    const int s = lane + 32 * i;
-    if (s < splits) ml[i] = *reinterpret_cast<const float2*>(part_ml + (s * pairs + pair) * 2);
-  }
-  float m = fmaxf(ml[0].x, ml[1].x);
-#pragma unroll
-  for (int st = 16; st > 0; st >>= 1) m = fmaxf(m, __shfl_xor(m, st));
-  float w[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) w[i] = ml[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[i].x - m);
-  const float* po = part_o + pair * kDh + lane * 4;
-  float l = 0.f;
+  const int lane = threadIdx.x & 63, hf = lane >> 5;
+  float2 ml = {-INFINITY, 0.f};
+  if (lane < splits) ml = *reinterpret_cast<const float2*>(part_ml + (lane * pairs + pair) * 2);
+  const float* po = part_o + pair * kDh + (lane & 31) * 4;
+  float w = 0.f, m = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < splits; s0 += 4) {
-    f32x4 v[4];
+  for (int s0 = 0; s0 < splits; s0 += 16) {
+    f32x4 v[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 8; ++i) {
+      const int s = s0 + 8 * hf + i;
       v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (s0 + i < splits) v[i] = *reinterpret_cast<const f32x4*>(po + (s0 + i) * pairs * kDh);
+      if (s < splits) v[i] = *reinterpret_cast<const f32x4*>(po + s * pairs * kDh);
+    }
+    if (s0 == 0) {  // behind the first loads
+      m = wave_max(ml.x);
+      w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int s = s0 + i;
-      const float ws = __shfl(s < 32 ? w[0] : w[1], s & 31, 32);
-      l += ws * __shfl(s < 32 ? ml[0].y : ml[1].y, s & 31, 32);
+    for (int i = 0; i < 8; ++i) {
+      const float ws = __shfl(w, (s0 + 8 * hf + i) & 63);
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[j] += ws * v[i][j];
     }
   }
+  const float l = wave_sum(w * ml.y);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) o[j] += __shfl_xor(o[j], 32);
+  if (hf) return;
   const float inv = 1.f / l;
   bf16x4 r;
 #pragma unroll
@@ -739,30 +738,41 @@ namespace {
 
 // Estimated time (us) of `units` (query tile, KV head) pairs over n_kt 64-key
 // tiles and the key splits that give it, within `fit`.  Measured: a launch and
-// its first loads 6; a step of the narrow kernel (32 keys a wave) 0.95, or 1.65
-// with two workgroups on a CU; a tile of the wide kernel 1.9, one workgroup a
-// CU; a merge 3.5 and its partials at 3 TB/s.
+// its first loads 6, 7.5 with two workgroups on a CU; a step of the narrow
+// kernel (32 keys a wave) 0.95, or 1.65 with two workgroups on a CU; a tile of
+// the wide kernel 1.9, one workgroup a CU; a merge 3.5 and its partials at 3
+// TB/s.  memory_us: the keys at 4.9 TB/s on all CUs, each request's read once;
+// below it more splits gain nothing.
+// Both sides of the choice, in us, narrow and wide at their best splits:
+//   32 rows, 32 heads, 1536 keys  11.6 / 12.0;  717 rows  38 / 41
+//   8 x 512 rows, 32 heads, 2432 keys  273 / 168
+//   4 x 32 rows, 28 heads on 4, 5120 keys  29.5 / 29.6;  4 x 256 rows  122 / 89
 struct Cost {
   double us;
   int splits;
 };
-Cost narrow_cost(int64_t units, int n_kt, int64_t pairs, int64_t fit) {
+double merge_us(int splits, int64_t pairs) {
+  return splits > 1 ? 3.5 + 2.0 * splits * pairs * (kDh + 2) * sizeof(float) / 3e6 : 0.0;
+}
+Cost narrow_cost(int64_t units, int n_kt, double memory_us, int64_t pairs, int64_t fit) {
   Cost best = {1e30, 1};
   for (int s = 1; s <= std::min<int64_t>(fit, kMaxSplits); ++s) {
-    const int64_t wgs = units * s, rounds = wgs / 512, rest = wgs % 512;
+    const int64_t wgs = units * s, rest = wgs % 512;
     const int steps = (2 * n_kt + kNwWaves * s - 1) / (kNwWaves * s);
-    const double us = 6.0 + steps * (1.65 * rounds + (rest == 0 ? 0.0 : rest <= 256 ? 0.95 : 1.65)) +
-                      (s > 1 ? 3.5 + 2.0 * s * pairs * (kDh + 2) * 4 / 3e6 : 0.0);
+    const double loop = steps * (1.65 * (wgs / 512) + (rest == 0 ? 0.0 : rest <= 256 ? 0.95 : 1.65));
+    const double memory = memory_us * 256.0 / std::min<int64_t>(wgs, 256);
+    const double us = (wgs <= 256 ? 6.0 : 7.5) + std::max(loop, memory) + merge_us(s, pairs);
     if (us < best.us) best = {us, s};
     if (steps == 1) break;
   }
   return best;
 }
-Cost wide_cost(int64_t units, int n_kt, int64_t pairs, int64_t fit) {
+Cost wide_cost(int64_t units, int n_kt, double memory_us, int64_t pairs, int64_t fit) {
   Cost best = {1e30, 1};
   for (int s = 1; s <= std::min<int64_t>(std::min<int64_t>(fit, kMaxSplits), std::max(n_kt, 1)); ++s) {
-    const double us = 6.0 + 1.9 * ((n_kt + s - 1) / s) * (double)((units * s + 255) / 256) +
-                      (s > 1 ? 3.5 + 2.0 * s * pairs * (kDh + 2) * 4 / 3e6 : 0.0);
+    const double loop = 1.9 * ((n_kt + s - 1) / s) * (double)((units * s + 255) / 256);
+    const double memory = memory_us * 256.0 / std::min<int64_t>(units * s, 256);
+    const double us = 6.0 + std::max(loop, memory) + merge_us(s, pairs);
     if (us < best.us) best = {us, s};
   }
   return best;
@@ -790,6 +800,7 @@ hipError_t launch_quant_attention(const Ragged& rg, int H, const QuantPool& p, c
   constexpr int kRest[3] = {64, 128, kWdTileQ - 1};
   int64_t narrow = 0, wide = 0, both_wide[3] = {}, both_narrow[3] = {};
   int n_kt = 0;
+  double memory_us = 0.0;
   for (int b = 0; b < rg.batch; ++b) {
     const int64_t n = (int64_t)(rg.cu_rows[b + 1] - rg.cu_rows[b]) * a.rep;
     narrow += (n + 31) / 32;
@@ -800,16 +811,18 @@ hipError_t launch_quant_attention(const Ragged& rg, int H, const QuantPool& p, c
       both_narrow[i] += few ? (n % kWdTileQ + 31) / 32 : 0;
     }
     n_kt = std::max(n_kt, (rg.cu_keys[b + 1] - rg.cu_keys[b] + kTileK - 1) / kTileK);
+    if (n > 0) memory_us += (rg.cu_keys[b + 1] - rg.cu_keys[b]) * (2.0 * kDh / 4.9e6) * p.heads;
   }
   const int64_t fit = std::max<int64_t>(1, (int64_t)(part_bytes / ((kDh + 2) * sizeof(float))) / pairs);
-  const Cost cn = narrow_cost(narrow * p.heads, n_kt, pairs, fit), cw = wide_cost(wide * p.heads, n_kt, pairs, fit);
+  const Cost cn = narrow_cost(narrow * p.heads, n_kt, memory_us, pairs, fit);
+  const Cost cw = wide_cost(wide * p.heads, n_kt, memory_us, pairs, fit);
   // the two launches write no partials: a merge would cover every row
   double both_us = 1e30;
   int both = 0;
   for (int i = 0; i < 3; ++i) {
     if (!both_wide[i] || !both_narrow[i]) continue;
-    const double us = wide_cost(both_wide[i] * p.heads, n_kt, pairs, 1).us +
-                      narrow_cost(both_narrow[i] * p.heads, n_kt, pairs, 1).us;
+    const double us = wide_cost(both_wide[i] * p.heads, n_kt, memory_us, pairs, 1).us +
+                      narrow_cost(both_narrow[i] * p.heads, n_kt, 0.0, pairs, 1).us;
     if (us < both_us) both_us = us, both = i;
   }
   // one launch over each request's queries: all of them, or those left to (or
@@ -842,7 +855,7 @@ hipError_t launch_quant_attention(const Ragged& rg, int H, const QuantPool& p, c
   const int splits = is_wide ? cw.splits : cn.splits;
   launch(is_wide, false, splits);
   if (splits > 1)
-    hipLaunchKernelGGL(quant_attention_merge_kernel, dim3((unsigned)((pairs + 7) / 8)), dim3(256), 0, s,
+    hipLaunchKernelGGL(quant_attention_merge_kernel, dim3((unsigned)((pairs + 3) / 4)), dim3(256), 0, s,
                        (const float*)a.part_o, (const float*)a.part_ml, splits, pairs, a.out, lse);
   return hipGetLastError();
 }
