@@ -128,9 +128,11 @@ struct StoreArgs {
   int n, heads, head_dim, shift;
 };
 
-// The last row of a run of rows in one block: a block's last row is one.
-__device__ __forceinline__ bool ends_run(const int32_t* slots, int i, int n, int shift) {
-  return i + 1 == n || (slots[i + 1] >> shift) != (slots[i] >> shift);
+// The last row of a run of rows in one block: a block's last row is one.  A row
+// without a slot ends a run too, also where its slot number lies in the short
+// last block.
+__device__ __forceinline__ bool ends_run(const int32_t* slots, int i, int n, int64_t n_slots, int shift) {
+  return i + 1 == n || slots[i + 1] >= n_slots || (slots[i + 1] >> shift) != (slots[i] >> shift);
 }
 
 // Leaves the last row of every slot that a call names, and of every block, in
@@ -153,7 +155,7 @@ __global__ __launch_bounds__(kThreads) void quant_map_kernel(const int32_t* __re
   const int i = (int)at, s = slots[i];
   if (s < 0 || s >= n_slots) return;
   keep_last(row_of + s, i, [&](int j) { return j >= 0 && j < n && slots[j] == s; });
-  if (ends_run(slots, i, n, shift))
+  if (ends_run(slots, i, n, n_slots, shift))
     keep_last(last_of + (s >> shift), i, [&](int j) { return j >= 0 && j < n && slots[j] >> shift == s >> shift; });
 }
 
@@ -251,7 +253,7 @@ __global__ __launch_bounds__(kThreads) void quant_store_kernel(StoreArgs<T> a) {
   __syncthreads();
   if (tid < block && tid < a.n - i0) {
     if constexpr (SMALL) {
-      if (all[i0 + tid] >= 0 && ends_run(all, i0 + tid, a.n, a.shift)) found[atomicAdd(&n_found, 1)] = i0 + tid;
+      if (all[i0 + tid] >= 0 && ends_run(all, i0 + tid, a.n, a.n_slots, a.shift)) found[atomicAdd(&n_found, 1)] = i0 + tid;
     } else {
       const int s = a.slots[i0 + tid];
       if (s >= 0 && s < a.n_slots && a.last_of[s >> a.shift] == i0 + tid) found[atomicAdd(&n_found, 1)] = s >> a.shift;

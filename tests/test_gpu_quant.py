@@ -118,6 +118,18 @@ def test_store_sizes(n, n_slots, order):
     p.store(slots[::-1].copy(), 4.0)
 
 
+@pytest.mark.parametrize("n", [200, 1500])
+def test_store_rows_past_the_short_last_block(n):
+    """Rows whose slot is not there, with numbers in the short last block's
+    range, behind and between the last rows of that block."""
+    n_slots = 32 * 64 + 20
+    p = Pair("bf16", 2, 128, n_slots, 64, seed=n)
+    slots = np.arange(n_slots - n, n_slots)
+    p.store(np.concatenate([slots, [n_slots, n_slots + 43]]))
+    p.store(np.concatenate([slots[:-5], [n_slots + 1], slots[-5:], [n_slots + 2, -1]]), 3.0)
+    p.store(np.concatenate([[n_slots], slots[::-1], [n_slots - 3, n_slots + 7, n_slots - 1, n_slots]]), 0.3)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_store_special_values(dtype):
     d = 128
