@@ -479,8 +479,9 @@ acache_status acache_linear(const acache_dims* dims, const void* a, const void* 
  * exponent, 3 significand bits, largest value 448, no infinity) with one
  * scale for every block of `block` consecutive slots and KV head.  An entry's
  * value is its code times its block's scale.  Scales are powers of two, so
- * the product is exact in bf16 and fp32; a scale of 0 marks an empty block,
- * whose slots read as zeros whatever their codes.  A new cache is made by
+ * the product is exact in bf16 and fp32 (a scale that a caller wrote itself is
+ * read as the power of two at or below it, of exponents -117 .. 119); a scale
+ * of 0 marks an empty block, whose slots read as zeros whatever their codes.  A new cache is made by
  * setting both scale arrays to zero; the codes need no initial value.
  * Clearing a block's scales empties it again, which a caller does when it
  * gives the block's slots to another request (otherwise the block keeps the
@@ -528,8 +529,7 @@ acache_status acache_quant_load(const acache_dims* dims, const acache_quant_pool
 /* acache_quant_attention — acache_attention over an 8-bit cache: the same
  * operation, layouts and ragged batch with K_j and V_j the cache's values
  * (a slot outside [0, n_slots) is a key and a value of zeros, as there).
- * bf16 only (ACACHE_ERR_UNSUPPORTED otherwise), n_slots * ld < 2^31.  Scales
- * other than powers of two are read as the power of two at or below them.
+ * bf16 only (ACACHE_ERR_UNSUPPORTED otherwise), n_slots * ld < 2^31.
  * ws is optional: with acache_quant_workspace_size(dims, rows, pool) bytes
  * the keys of calls with few rows are split over workgroups (fp32 partials,
  * combined in a fixed order); with less, in fewer parts or none. */

@@ -315,7 +315,7 @@ __global__ __launch_bounds__(kThreads) void quant_load_kernel(const uint8_t* __r
 #pragma unroll
     for (int j = 0; j < 16; ++j) v[j] = 0.f;
     if (s >= 0 && s < n_slots) {
-      const float sc = scales[(int64_t)(s >> shift) * heads + c / per_head];
+      const float sc = pow2_below(scales[(int64_t)(s >> shift) * heads + c / per_head]);
       if (sc > 0.f) {
         const u32x4 w = *reinterpret_cast<const u32x4*>(codes + (int64_t)s * ld + c * 16);
 #pragma unroll

@@ -506,7 +506,7 @@ __global__ __launch_bounds__(64 * kNwWaves, 2) void quant_attention_narrow_kerne
   };
   auto put_scales = [&](const Scales& x) {
     *reinterpret_cast<uint32_t*>(k_scales + lane * 4) = x.k;
-    *reinterpret_cast<uint32_t*>(v_scales + lane * 4) = x.v;
+    *reinterpret_cast<float*>(v_scales + lane * 4) = pow2_below(__uint_as_float(x.v));
     return __builtin_amdgcn_ballot_w64(!(__uint_as_float(x.k) > 0.f) || !(__uint_as_float(x.v) > 0.f)) != 0;
   };
   const int lrow = lane >> 3, lch = lane & 7;

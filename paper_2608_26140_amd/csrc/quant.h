@@ -23,6 +23,10 @@ __device__ __forceinline__ int scale_byte(float amax) {
   return min(max(b, kMinScaleByte), kMaxScaleByte);
 }
 __device__ __forceinline__ float pow2_byte(int b) { return __uint_as_float((uint32_t)b << 23); }
+// A scale as it is read: the power of two at or below it.
+__device__ __forceinline__ float pow2_below(float scale) {
+  return __uint_as_float(__float_as_uint(scale) & 0xFF800000u);
+}
 
 // Four codes of x * inv, rounded to nearest even; an infinity or a NaN gives
 // NaN (e4m3 has no infinity).

@@ -349,6 +349,33 @@ def test_attention_extreme_scales(rows):
     run_attention(p, [rows], [320], np.arange(320), q=q, what="extreme")
 
 
+def test_scales_are_read_as_powers_of_two():
+    """Scales of any significand give the bits of the powers of two at or below
+    them, in every reader and in a store that keeps entries."""
+    p = filled(4, 4, 600, 32, seed=23)
+    slots = up_i32(p.rng.permutation(600))
+    q = [torch.randn(r, 512, device=DEV).to(torch.bfloat16) for r in (1, 64 * 256)]
+    new = [torch.randn(9, 512, device=DEV).to(torch.bfloat16) for _ in range(2)]
+
+    def read():
+        one = A.acache_quant_attention(p.dims, [0, 1], [0, 600], q[0], slots, p.pool, ws=p.ws)
+        many = A.acache_quant_attention(p.dims, np.arange(65) * 256, np.arange(65) * 9, q[1], slots, p.pool)
+        return (one, many, *A.acache_quant_load(p.dims, p.pool, slots))
+
+    def store():
+        A.acache_quant_store(p.dims, p.pool, *new, slots[:9].contiguous(), ws=p.ws)
+        return read()
+    state = [t.clone() for t in (*p.dev, p.pool.k_scales, p.pool.v_scales)]
+    want = read(), store()
+    for t, was in zip((*p.dev, p.pool.k_scales, p.pool.v_scales), state):
+        t.copy_(was)
+    for t in (p.pool.k_scales, p.pool.v_scales):
+        t.mul_(1.0 + 0.999 * torch.rand(t.shape, device=DEV))
+    got = read(), store()
+    for w, g in zip(want, got):
+        assert all(torch.equal(a, b) for a, b in zip(w, g))
+
+
 @pytest.mark.parametrize("rows", [1, 40, 300])
 def test_attention_nan_shows(rows):
     """A NaN key makes every row that reads it NaN; other heads and requests stay."""
