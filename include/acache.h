@@ -514,8 +514,9 @@ typedef struct {
  * that name one slot the last is stored.  Rows whose slot is outside
  * [0, n_slots) are skipped.  Untouched blocks keep every bit.  The result
  * does not depend on the order of the work: identical inputs give identical
- * bits.  ws: at least acache_quant_workspace_size(dims, 0, pool) bytes, no
- * initial contents needed.  n == 0: no-op. */
+ * bits.  (n / block + 1) * H_kv < 2^23 (ACACHE_ERR_UNSUPPORTED otherwise).  ws:
+ * at least acache_quant_workspace_size(dims, 0, pool) bytes, no initial contents
+ * needed.  n == 0: no-op. */
 acache_status acache_quant_store(const acache_dims* dims, const acache_quant_pool* pool, const void* k_src,
                                  const void* v_src, int64_t src_ld, int32_t n, const int32_t* dst_slots, void* ws,
                                  size_t ws_bytes, hipStream_t stream);
@@ -529,7 +530,8 @@ acache_status acache_quant_load(const acache_dims* dims, const acache_quant_pool
 /* acache_quant_attention — acache_attention over an 8-bit cache: the same
  * operation, layouts and ragged batch with K_j and V_j the cache's values
  * (a slot outside [0, n_slots) is a key and a value of zeros, as there).
- * bf16 only (ACACHE_ERR_UNSUPPORTED otherwise), n_slots * ld < 2^31.
+ * bf16 only (ACACHE_ERR_UNSUPPORTED otherwise), n_slots * ld < 2^31, at most
+ * 2^28 rows times heads and 2^29 keys of a request.
  * ws is optional: with acache_quant_workspace_size(dims, rows, pool) bytes
  * the keys of calls with few rows are split over workgroups (fp32 partials,
  * combined in a fixed order); with less, in fewer parts or none. */
@@ -548,7 +550,7 @@ size_t acache_quant_workspace_size(const acache_dims* dims, int32_t max_rows, co
  * set, the affix keys of Eq. 4 are the cache's values; the score makes its own
  * pass over them (affix_keys_known is not used).  write_slots, read_slots and
  * the other arguments, shapes and errors are those of acache_layer_recompute;
- * bf16 only, n_slots * ld < 2^31.  A decode step (Section 4.3) is this call
+ * bf16 only, with the limits of acache_quant_attention.  A decode step (Section 4.3) is this call
  * with the block's rows, their slots and the refresh's read_slots.  ws: at
  * least acache_quant_layer_workspace_size(dims, rows, batch, L, pool) bytes
  * (a workspace of more rows, requests and affix keys serves smaller calls). */

@@ -946,6 +946,14 @@ static acache_status check_quant_buffers(const QuantPool& p) {
   return ACACHE_OK;
 }
 
+// Requests of the 8-bit attention: 32-bit byte offsets into a request's read
+// slots, those read ahead included, and a launch of fewer than 2^32 threads.
+static acache_status check_quant_ragged(const Ragged& r, int heads) {
+  CHECK((int64_t)r.cu_rows[r.batch] * heads <= ((int64_t)1 << 28), ACACHE_ERR_UNSUPPORTED);
+  for (int b = 0; b < r.batch; ++b) CHECK(r.cu_keys[b + 1] - r.cu_keys[b] <= (1 << 29), ACACHE_ERR_UNSUPPORTED);
+  return ACACHE_OK;
+}
+
 size_t acache_quant_workspace_size(const acache_dims* dims, int32_t max_rows, const acache_quant_pool* pool) {
   QuantPool p;
   if (check_quant_pool(dims, pool, p) != ACACHE_OK || max_rows < 0) return 0;
@@ -967,8 +975,8 @@ acache_status acache_quant_store(const acache_dims* dims, const acache_quant_poo
   const int64_t es = (int64_t)elem_size(dims->dtype);
   CHECK(src_ld >= (int64_t)p.heads * p.head_dim, ACACHE_ERR_SHAPE);
   CHECK(aligned16(k_src) && aligned16(v_src) && (src_ld * es) % 16 == 0, ACACHE_ERR_ALIGN);
-  // a workgroup for every `block` rows, K and V of every head
-  CHECK(((int64_t)n / pool->block + 1) * 2 * p.heads < ((int64_t)1 << 31), ACACHE_ERR_UNSUPPORTED);
+  // a workgroup of 256 threads for every `block` rows, K and V of every head: fewer than 2^32 threads
+  CHECK(((int64_t)n / pool->block + 1) * 2 * p.heads < ((int64_t)1 << 24), ACACHE_ERR_UNSUPPORTED);
   CHECK(ws && ((uintptr_t)ws & 3u) == 0 && ws_bytes >= quant_map_bytes(p.n_slots, p.shift), ACACHE_ERR_WORKSPACE);
   LAUNCH_T(ACACHE_K_SCATTER, stream,
            launch_quant_store(dims->dtype, p, k_src, v_src, src_ld, n, dst_slots, (int32_t*)ws, stream));
@@ -1007,7 +1015,8 @@ acache_status acache_quant_attention(const acache_dims* dims, const acache_ragge
   st = check_quant_buffers(p);
   if (st != ACACHE_OK) return st;
   CHECK(p.n_slots * p.ld < ((int64_t)1 << 31), ACACHE_ERR_UNSUPPORTED);  // 32-bit offsets
-  CHECK((int64_t)r.cu_rows[r.batch] * dims->n_heads < ((int64_t)1 << 31), ACACHE_ERR_UNSUPPORTED);
+  st = check_quant_ragged(r, dims->n_heads);
+  if (st != ACACHE_OK) return st;
   CHECK(aligned16(q) && aligned16(out), ACACHE_ERR_ALIGN);
   CHECK(!ws || aligned16(ws), ACACHE_ERR_ALIGN);
   LAUNCH_T(ACACHE_K_ATTENTION, stream,
@@ -1071,6 +1080,8 @@ acache_status acache_quant_layer_recompute(const acache_dims* dims, const acache
   const int hq = H * dh, hkv = Hkv * dh, nqkv = (H + 2 * Hkv) * dh;
   CHECK(p.n_slots > 0, ACACHE_ERR_SHAPE);
   CHECK(p.n_slots * p.ld < ((int64_t)1 << 31), ACACHE_ERR_UNSUPPORTED);  // 32-bit offsets
+  st = check_quant_ragged(r, H);
+  if (st != ACACHE_OK) return st;
   CHECK((int64_t)M * std::max({d, hq, hkv, F}) < ((int64_t)1 << 31), ACACHE_ERR_UNSUPPORTED);
   CHECK((int64_t)std::max({nqkv, 2 * F, d}) * std::max({d, hq, F}) < ((int64_t)1 << 31), ACACHE_ERR_UNSUPPORTED);
   CHECK(aligned16(x), ACACHE_ERR_ALIGN);

@@ -130,6 +130,33 @@ def test_attention_refusals(A):
     assert call(desc=pool(A, n_slots=1 << 20)) == 4  # 2^20 rows of 4096 bytes: past 32-bit offsets
 
 
+def test_sizes_past_a_launch_are_refused(A):
+    """A launch holds fewer than 2^32 threads, a request's slots lie within 32-bit byte offsets."""
+    lib, dims, p = A.lib, A.make_dims(*DIMS), ctypes.c_void_p(16)
+    d = ctypes.byref(dims)
+    big = 1 << 40
+
+    def store(n, block):
+        return lib.acache_quant_store(d, ctypes.byref(pool(A, block=block)), p, p, 4096, n, p, None, big, None)
+    assert store(1 << 22, 16) == 4 and store((1 << 22) - 17, 16) == 5  # 5: the missing workspace, checked next
+    assert store((1 << 26) - 300, 256) == 5 and store(1 << 26, 256) == 4
+
+    def attend(rows, keys):
+        rg, keep = A._ragged(rows, keys)
+        return lib.acache_quant_attention(d, ctypes.byref(rg), p, p, ctypes.byref(pool(A)), p, None, ctypes.c_void_p(8),
+                                          0, None)
+    assert attend((0, 1 << 23), (0, 5)) == 3 and attend((0, (1 << 23) + 1), (0, 5)) == 4  # 3: the workspace's alignment
+    assert attend((0, 1, 2), (0, 5, 5 + (1 << 29))) == 3 and attend((0, 1, 2), (0, 5, 6 + (1 << 29))) == 4
+    assert attend((0, 1), (0, (1 << 31) - 1)) == 4
+
+    def layer(rows, keys):
+        rg, keep = A._ragged(rows, keys)
+        lw = A.LayerWeights(*[16] * len(A.LayerWeights._fields_))
+        return lib.acache_quant_layer_recompute(d, ctypes.byref(lw), ctypes.byref(rg), p, p, p, p, ctypes.byref(pool(A)),
+                                                None, None, 0, None)
+    assert layer((0, 3), (0, 1 << 29)) == 5 and layer((0, 3), (0, (1 << 29) + 1)) == 4
+
+
 def test_workspace_size(A):
     lib, dims = A.lib, A.make_dims(*DIMS)
 
