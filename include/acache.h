@@ -550,10 +550,11 @@ size_t acache_quant_workspace_size(const acache_dims* dims, int32_t max_rows, co
  * set, the affix keys of Eq. 4 are the cache's values; the score makes its own
  * pass over them (affix_keys_known is not used).  write_slots, read_slots and
  * the other arguments, shapes and errors are those of acache_layer_recompute;
- * bf16 only, with the limits of acache_quant_attention.  A decode step (Section 4.3) is this call
- * with the block's rows, their slots and the refresh's read_slots.  ws: at
- * least acache_quant_layer_workspace_size(dims, rows, batch, L, pool) bytes
- * (a workspace of more rows, requests and affix keys serves smaller calls). */
+ * bf16 only, with the limits of acache_quant_attention.  A decode step
+ * (Section 4.3) is this call with the block's rows, their slots and the
+ * refresh's read_slots.  ws: at least
+ * acache_quant_layer_workspace_size(dims, rows, batch, L, pool) bytes (a
+ * workspace of more rows, requests and affix keys serves smaller calls). */
 acache_status acache_quant_layer_recompute(const acache_dims* dims, const acache_layer_weights* w,
                                            const acache_ragged* rg, void* x, const int32_t* pos,
                                            const int32_t* write_slots, const int32_t* read_slots,

@@ -9,6 +9,7 @@ tensors used as device memory.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional, Sequence
@@ -577,6 +578,11 @@ def quant_workspace(dims: Dims, max_rows: int, pool: QuantPool) -> torch.Tensor:
     return torch.empty(acache_quant_workspace_size(dims, max_rows, pool), dtype=torch.uint8, device=pool.device)
 
 
+def _own(stream):
+    """Tensors made inside belong to the stream that a call uses them on."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
 def _quant_check(dims: Dims, pool: QuantPool, *tensors):
     """The pool fits dims, and everything is on the current device."""
     if pool.heads != dims.n_kv_heads or pool.width < dims.n_kv_heads * dims.head_dim:
@@ -609,7 +615,8 @@ def acache_quant_store(dims: Dims, pool: QuantPool, k_src: torch.Tensor, v_src: 
     n = dst_slots.numel()
     ld = _quant_rows(dims, k_src, v_src, n)
     if ws is None:
-        ws = quant_workspace(dims, 0, pool)
+        with _own(stream):
+            ws = quant_workspace(dims, 0, pool)
     _quant_check(dims, pool, k_src, v_src, dst_slots, ws)
     _check("acache_quant_store", lib.acache_quant_store(
         ctypes.byref(dims), pool.ref, k_src.data_ptr(), v_src.data_ptr(), ld, n, dst_slots.data_ptr(), ws.data_ptr(),
@@ -623,8 +630,9 @@ def acache_quant_load(dims: Dims, pool: QuantPool, slots: torch.Tensor, k_out: O
     _dev_i32(slots, "slots")
     n = slots.numel()
     if k_out is None and v_out is None:
-        k_out = torch.empty((n, dims.n_kv_heads * dims.head_dim), dtype=torch_dtype(dims), device=slots.device)
-        v_out = torch.empty_like(k_out)
+        with _own(stream):
+            k_out = torch.empty((n, dims.n_kv_heads * dims.head_dim), dtype=torch_dtype(dims), device=slots.device)
+            v_out = torch.empty_like(k_out)
     k, v = k_out if k_out is not None else v_out, v_out if v_out is not None else k_out
     ld = _quant_rows(dims, k, v, n)
     _quant_check(dims, pool, slots, k, v)
@@ -641,7 +649,8 @@ def acache_quant_attention(dims: Dims, cu_rows, cu_keys, q: torch.Tensor, read_s
     _dev_i32(read_slots, "read_slots")
     rg, keep = _ragged(cu_rows, cu_keys)
     if out is None:
-        out = torch.empty_like(q)
+        with _own(stream):
+            out = torch.empty_like(q)
     rows, width = int(cu_rows[-1]), dims.n_heads * dims.head_dim
     for t, name in ((q, "q"), (out, "out")):
         if t.dtype != torch_dtype(dims) or t.numel() < rows * width or not t.is_contiguous():

@@ -211,6 +211,34 @@ def test_load_one_of_two_and_strided():
     assert (wide[:, :512] == 3).all() and (wide[:, 768:] == 3).all()
 
 
+def test_stream_of_workspace_and_results():
+    """What a call on another stream makes for itself is that stream's: neither
+    its workspace nor its results use memory that the current stream still
+    works with, and the workspace is not given away before the call has run."""
+    p = Pair("bf16", 2, 128, 4000, 64, seed=6)
+    slots = p.rng.permutation(4000)[:3000]
+    x = [p.rng.normal(0, 1, (3000, 2, 128)) for _ in range(2)]
+    src = [rows_of(v, "bf16") for v in x]
+    dst = up_i32(slots)
+    for r, (_, v64) in zip(p.ref, src):
+        r.store(v64, slots)
+    other = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    A.acache_quant_store(p.dims, p.pool, src[0][0], src[1][0], dst, stream=other)
+    scrap = [torch.full((5000,), 7, dtype=torch.int32, device=DEV) for _ in range(8)]  # the current stream's
+    k, v = A.acache_quant_load(p.dims, p.pool, dst, stream=other)
+    q = torch.randn(40, 256, device=DEV).to(torch.bfloat16)
+    torch.cuda.current_stream().synchronize()
+    lse = torch.empty(40, 2, device=DEV)
+    out = A.acache_quant_attention(p.dims, [0, 40], [0, 3000], q, dst, p.pool, lse=lse, stream=other)
+    torch.cuda.synchronize()
+    p.check()
+    for got, ref in ((k, p.ref[0]), (v, p.ref[1])):
+        np.testing.assert_array_equal(got.double().cpu().numpy().reshape(3000, 2, 128), ref.values(slots))
+    check_attention(p, q, [0, 40], [0, 3000], slots, out, lse, "another stream")
+    assert all((t == 7).all() for t in scrap)
+
+
 # ---------------------------------------------------------------------------- attention
 def check_attention(p, q, cu_rows, cu_keys, slots, out, lse, what=""):
     H, Hkv, d = p.dims.n_heads, p.Hkv, p.d
