@@ -427,6 +427,13 @@ __global__ __launch_bounds__(kWdThreads, 1) void quant_attention_wide_kernel(QAt
 // instead.  16-byte chunk c of row r lies at c ^ k_swizzle(r) (K) and
 // c ^ (r & 7) (V).  Slots are read and offsets and scales made for 64 keys at a
 // time, one key a lane.
+// Measured: keys that one request alone reads at 5.1 TB/s, the rate of a large
+// copy, with all CUs busy (a query of 8 requests over 30,000 keys of 4 heads:
+// 48 us); keys that lie in the caches 0.95 us a tile of 32 for a wave, which is
+// its conversions, products and weights one after the other.  32 rows of each
+// of 32 requests, 32 heads, over 8704 keys take 233 us; with codes copied
+// straight to LDS 247, with the loop software pipelined 238, with neighbouring
+// heads side by side in the grid 281.
 // ============================================================================
 constexpr int kNwWaves = 4;
 constexpr int kNwTileK = 32;
@@ -681,7 +688,8 @@ __global__ __launch_bounds__(64 * kNwWaves, 2) void quant_attention_narrow_kerne
 // 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  A wave per (row, head): lane s holds
 // split s's max and sum; lane half hf sums 4 dimensions a lane over the splits
 // s with (s / 8) % 2 == hf, in order, eight loads in flight at a time (a chain
-// of loads is what bounds it), and the halves are added last.
+// of loads is what bounds it), and the halves are added last.  1024 pairs of six
+// splits add 2.5 us to the call (4 with a load at a time).
 __global__ __launch_bounds__(256) void quant_attention_merge_kernel(const float* __restrict__ part_o,
                                                                     const float* __restrict__ part_ml, int splits,
                                                                     int64_t pairs, bf16* __restrict__ out,
