@@ -143,8 +143,10 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _stream(stream=None):
-    # with the device's index current_stream skips its search for a device (1 us)
-    return (stream if stream is not None else torch.cuda.current_stream(torch.cuda.current_device())).cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    # the handle alone: a Stream object around it costs another microsecond
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _i32(values: Sequence[int]):
@@ -578,9 +580,12 @@ def quant_workspace(dims: Dims, max_rows: int, pool: QuantPool) -> torch.Tensor:
     return torch.empty(acache_quant_workspace_size(dims, max_rows, pool), dtype=torch.uint8, device=pool.device)
 
 
+_HERE = contextlib.nullcontext()
+
+
 def _own(stream):
     """Tensors made inside belong to the stream that a call uses them on."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+    return _HERE if stream is None else torch.cuda.stream(stream)
 
 
 def _quant_check(dims: Dims, pool: QuantPool, *tensors):
