@@ -158,8 +158,11 @@ __global__ __launch_bounds__(kThreads) void quant_map_kernel(const int32_t* __re
   const int i = (int)at, s = slots[i];
   if (s < 0 || s >= n_slots) return;
   keep_last(row_of + s, i, [&](int j) { return j >= 0 && j < n && slots[j] == s; });
+  // a stale entry may name a row whose slot number lies in the short last block
+  // past its end: that row is stored nowhere and must not stand for the block
   if (ends_run(slots, i, n, n_slots, shift))
-    keep_last(last_of + (s >> shift), i, [&](int j) { return j >= 0 && j < n && slots[j] >> shift == s >> shift; });
+    keep_last(last_of + (s >> shift), i,
+              [&](int j) { return j >= 0 && j < n && slots[j] < n_slots && slots[j] >> shift == s >> shift; });
 }
 
 // Quantises one block and head from its map win (LDS): the row stored at each
