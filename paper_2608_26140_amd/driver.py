@@ -343,10 +343,10 @@ class AffixBatch:
 
     def full_refresh(self, stream=None):
         every = torch.arange(self.L, dtype=torch.int32, device=self.device).repeat(self.B, 1).contiguous()
-        return self.refresh(every, self.L, stream)
+        return self.refresh(every, self.L, stream=stream)
 
     def direct_reuse(self, stream=None):
-        return self.refresh(None, 0, stream)
+        return self.refresh(None, 0, stream=stream)
 
 
 class Head:
