@@ -558,12 +558,15 @@ class QuantPool:
             t[first:max(first, last)].zero_()
 
 
-def quant_pool(dims: Dims, n_slots: int, block: int = 64, device="cuda") -> QuantPool:
-    """An empty 8-bit cache of n_slots slots."""
+def quant_pool(dims: Dims, n_slots: int, block: int = 64, device="cuda",
+               scales: Optional[Sequence[torch.Tensor]] = None) -> QuantPool:
+    """An empty 8-bit cache of n_slots slots.  scales: K's and V's, of zeros
+    (a caller's that keeps several caches' in one tensor); None makes them."""
     row = dims.n_kv_heads * dims.head_dim
     codes = [torch.empty((n_slots, row), dtype=torch.uint8, device=device) for _ in range(2)]
-    scales = [torch.zeros((-(-n_slots // block), dims.n_kv_heads), dtype=torch.float32, device=device)
-              for _ in range(2)]
+    if scales is None:
+        scales = [torch.zeros((-(-n_slots // block), dims.n_kv_heads), dtype=torch.float32, device=device)
+                  for _ in range(2)]
     return QuantPool(*codes, *scales, block)
 
 

@@ -68,7 +68,10 @@ class AffixBatch:
     quant_block slots and KV head; bf16 models.  The affix and each request's
     private slots then begin on a scale's block (the paged plan's block_size
     has to be a multiple of quant_block), so that no request's entries share a
-    scale with another's."""
+    scale with another's.  Every run of the layers over a batch's rows (a
+    probe, a refresh) empties the private blocks first, so that none shares
+    one with what the slots held before either; the decode steps behind a
+    refresh keep its entries."""
 
     def __init__(self, model: Model, seq_len: int, affix_begin: int, affix_len: int, mask_begin: int,
                  mask_len: int, batch: int, x_src: torch.Tensor, remap: Optional[torch.Tensor] = None,
@@ -107,7 +110,13 @@ class AffixBatch:
             self.affix_slots = torch.arange(affix_len, dtype=torch.int32, device=device)
         self.quant_block = quant_block
         if quant_block:
-            self.caches = [A.quant_pool(model.dims, self.n_slots, quant_block, device) for _ in range(model.n_layers)]
+            # all layers' scales [layer, K and V, block, head] in one tensor: what is emptied together is one
+            # fill.  No affix entry lies from block first_private on, and every private one does.
+            self.scales = torch.zeros((model.n_layers, 2, -(-self.n_slots // quant_block), model.dims.n_kv_heads),
+                                      dtype=torch.float32, device=device)
+            self.first_private = (self.private_base if self.pages is None else n_shared * block_size) // quant_block
+            self.caches = [A.quant_pool(model.dims, self.n_slots, quant_block, device, scales=sc)
+                           for sc in self.scales]
             self.k_pools, self.v_pools = [], []
             self.ws = A.quant_layer_workspace(model.dims, batch * r_max, batch, affix_len, self.caches[0])
         else:
@@ -219,6 +228,11 @@ class AffixBatch:
         if score is not None and len(groups) > 1:
             raise ValueError("probe batch too large for one call")
         n_run = self.model.n_layers if upto is None else min(upto, self.model.n_layers)
+        if self.quant_block:
+            # every private entry that these rows read they write first; what else the blocks hold, and its
+            # scales, belongs to an earlier run, maybe of another request
+            with _on(stream):
+                self.scales[:, :, self.first_private:].zero_()
         for n in range(n_run):
             if layer_hook is not None:
                 layer_hook(n, x)
