@@ -542,7 +542,7 @@ class QuantPool:
                                   ld, k_codes.shape[0], block)
         self.ref = ctypes.byref(self.desc)
 
-    def clear(self, slots: Optional[slice] = None):
+    def clear(self, slots: Optional[slice] = None, stream=None):
         """Empties every block (slots None) or those that lie wholly in the
         given slots: their entries read as zeros."""
         if slots is None:
@@ -554,8 +554,9 @@ class QuantPool:
             first, last = -(-start // self.block), stop // self.block
             if stop == self.k_codes.shape[0]:
                 last = self.k_scales.shape[0]
-        for t in (self.k_scales, self.v_scales):
-            t[first:max(first, last)].zero_()
+        with _own(stream):
+            for t in (self.k_scales, self.v_scales):
+                t[first:max(first, last)].zero_()
 
 
 def quant_pool(dims: Dims, n_slots: int, block: int = 64, device="cuda",
@@ -587,7 +588,8 @@ _HERE = contextlib.nullcontext()
 
 
 def _own(stream):
-    """Tensors made inside belong to the stream that a call uses them on."""
+    """Tensors made inside belong to the stream that a call uses them on, and
+    torch's fills run on it."""
     return _HERE if stream is None else torch.cuda.stream(stream)
 
 
