@@ -15,12 +15,32 @@ on one stream, without synchronising.
 from __future__ import annotations
 
 import contextlib
+import functools
+import inspect
 from typing import Callable, List, Optional
 
 import numpy as np
 import torch
 
 from . import acache as A
+
+
+def _on(stream):
+    """torch's own copies and fills go to the stream the library calls use."""
+    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+
+
+def _on_its_stream(call):
+    """A call with a `stream` makes every tensor on it, temporaries and results:
+    one made on the current stream could be read before that stream has filled
+    it, and be given away while the call's kernels still work with it."""
+    at = list(inspect.signature(call).parameters).index("stream")
+
+    @functools.wraps(call)
+    def wrapped(*args, **kwargs):
+        with _on(args[at] if len(args) > at else kwargs.get("stream")):
+            return call(*args, **kwargs)
+    return wrapped
 
 
 class Model:
@@ -173,6 +193,7 @@ class AffixBatch:
     def rows_per_request(self, k: int) -> int:
         return k + self.S - self.L
 
+    @_on_its_stream
     def maps(self, anchors: Optional[torch.Tensor], k: int, stream=None, key_order: int = 0) -> dict:
         """key_order 1: each request's read slots list the affix keys first
         (the probe's order; see acache_layout.key_order)."""
@@ -186,6 +207,7 @@ class AffixBatch:
         return A.acache_build_maps_paged(lay, self.B, anchors, k, self.bs, self.shared_blocks, tbl, nb,
                                          self.device, stream)
 
+    @_on_its_stream
     def gather_inputs(self, m: dict, stream=None) -> torch.Tensor:
         return A.acache_gather_rows(self.x_src, m["row_src"], self.remap, stream=stream)
 
@@ -209,6 +231,7 @@ class AffixBatch:
             A.acache_layer_recompute(dims, lw, cu_rows, cu_keys, x, pos, write_slots, read_slots, self.k_pools[n],
                                      self.v_pools[n], self.ws, score=score, stream=stream)
 
+    @_on_its_stream
     def run_layers(self, x: torch.Tensor, m: dict, k: int, score: Optional[dict] = None,
                    drop_non_anchor: bool = False, upto: Optional[int] = None, score_last_only: bool = False,
                    stream=None, layer_hook: Optional[Callable[[int, torch.Tensor], None]] = None):
@@ -231,8 +254,7 @@ class AffixBatch:
         if self.quant_block:
             # every private entry that these rows read they write first; what else the blocks hold, and its
             # scales, belongs to an earlier run, maybe of another request
-            with _on(stream):
-                self.scales[:, :, self.first_private:].zero_()
+            self.scales[:, :, self.first_private:].zero_()
         for n in range(n_run):
             if layer_hook is not None:
                 layer_hook(n, x)
@@ -256,6 +278,7 @@ class AffixBatch:
         return x
 
     # ------------------------------------------------------------------ the method
+    @_on_its_stream
     def materialize_affix(self, donor_x: torch.Tensor, donor_pos: torch.Tensor, write_slots: torch.Tensor,
                           read_slots: torch.Tensor, stream=None) -> torch.Tensor:
         """Materialise the shared affix cache once (Sections 3.3, 4.2): a full
@@ -268,24 +291,24 @@ class AffixBatch:
                                  stream=stream)
         return donor_x
 
+    @_on_its_stream
     def shift_affix(self, delta: int, stream=None):
         """Reuse the shared affix cache delta positions from where it was
         materialised: its K rows are re-rotated in place at every layer (8-bit
         caches: read back, turned and stored again)."""
         slots = self.affix_slots
-        with _on(stream):
-            d = torch.full((self.L,), int(delta), dtype=torch.int32, device=self.device)
-            rows = torch.arange(self.L, dtype=torch.int32, device=self.device)
+        d = torch.full((self.L,), int(delta), dtype=torch.int32, device=self.device)
+        rows = torch.arange(self.L, dtype=torch.int32, device=self.device)
         for c in self.caches:
-            with _on(stream):
-                k, v = (torch.empty((self.L, self.model.kv_width), dtype=self.model.dtype, device=self.device)
-                        for _ in range(2))
+            k, v = (torch.empty((self.L, self.model.kv_width), dtype=self.model.dtype, device=self.device)
+                    for _ in range(2))
             A.acache_quant_load(self.model.dims, c, slots, k, v, stream=stream)
             A.acache_rerotate_k(self.model.dims, k, rows, k, rows, d, stream=stream)
             A.acache_quant_store(self.model.dims, c, k, v, slots, ws=self.ws, stream=stream)
         for k in self.k_pools:
             A.acache_rerotate_k(self.model.dims, k, slots, k, slots, d, stream=stream)
 
+    @_on_its_stream
     def probe(self, norm: int = A.ACACHE_NORM_AFFIX, stream=None, outputs: bool = True, layer_hook=None,
               attention_lse: bool = True):
         """One-shot probe (Section 3.2): forward the non-affix rows against the
@@ -316,6 +339,7 @@ class AffixBatch:
         self.run_layers(x, m, 0, score=score, score_last_only=not outputs, stream=stream, layer_hook=hook)
         return scores, (x if outputs else None), m
 
+    @_on_its_stream
     def select_anchors(self, k: int, norm: int = A.ACACHE_NORM_AFFIX, stream=None, full_probe: bool = False):
         """Probe then Eq. 6.  Returns (anchors [B, k] int32 ascending, scores).
         The probe's last layer stops at its score unless full_probe."""
@@ -324,6 +348,7 @@ class AffixBatch:
             return torch.empty((self.B, 0), dtype=torch.int32, device=self.device), scores
         return A.acache_topk(scores, k, stream=stream), scores
 
+    @_on_its_stream
     def select_anchors_hkvd(self, k: int, stream=None):
         """The CacheBlend-style selector (KV deviation) in place of Eq. 4-5:
         a full-prompt forward of every request through the selection layer
@@ -345,6 +370,7 @@ class AffixBatch:
             return torch.empty((self.B, 0), dtype=torch.int32, device=self.device), scores
         return A.acache_topk(scores, k, stream=stream), scores
 
+    @_on_its_stream
     def refresh(self, anchors: Optional[torch.Tensor], k: int, drop_non_anchor: bool = False, stream=None,
                 layer_hook=None):
         """Selective recomputation (Section 3.3): anchors plus every
@@ -355,10 +381,12 @@ class AffixBatch:
         self.run_layers(x, m, k, drop_non_anchor=drop_non_anchor, stream=stream, layer_hook=layer_hook)
         return x, m
 
+    @_on_its_stream
     def full_refresh(self, stream=None):
         every = torch.arange(self.L, dtype=torch.int32, device=self.device).repeat(self.B, 1).contiguous()
         return self.refresh(every, self.L, stream=stream)
 
+    @_on_its_stream
     def direct_reuse(self, stream=None):
         return self.refresh(None, 0, stream=stream)
 
@@ -421,6 +449,7 @@ class DecodePlan:
         return self._slots[blk]
 
 
+@_on_its_stream
 def decode_schedule(batch: AffixBatch, head: Head, plan: DecodePlan, k: int, logits: torch.Tensor,
                     committed: torch.Tensor, anchors: Optional[torch.Tensor] = None, stream=None):
     """The serving schedule over the masked span (Sections 3.1 and 4.3): one
@@ -463,11 +492,7 @@ def capture(fn, warmup: int = 2):
     return g, out
 
 
-def _on(stream):
-    """torch's own copies and fills go to the stream the library calls use."""
-    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
-
-
+@_on_its_stream
 def decode_step(batch: AffixBatch, plan: DecodePlan, blk: int, m: dict, anchors: Optional[torch.Tensor] = None,
                 split_shared: bool = True, stream=None):
     """One decoding step of block ``blk`` (Section 4.3, Appendix C.1): the
@@ -500,6 +525,7 @@ def decode_step(batch: AffixBatch, plan: DecodePlan, blk: int, m: dict, anchors:
     return h
 
 
+@_on_its_stream
 def decode_threshold_schedule(batch: AffixBatch, head: Head, plan: DecodePlan, k: int, tau: float,
                               anchors: Optional[torch.Tensor] = None, trace: Optional[list] = None,
                               max_steps: Optional[int] = None, stream=None):
@@ -542,8 +568,7 @@ def decode_threshold_schedule(batch: AffixBatch, head: Head, plan: DecodePlan, k
     for blk in range(plan.n_blocks):
         x, m = batch.refresh(anchors, plan.k, stream=stream)
         h = A.acache_gather_rows(x, plan.rows[blk], stream=stream)
-        with _on(stream):
-            flags.zero_()
+        flags.zero_()
         done, step = 0, 0
         while True:
             y = A.acache_rmsnorm(dims, h, head.norm_g, stream=stream)
@@ -551,9 +576,8 @@ def decode_threshold_schedule(batch: AffixBatch, head: Head, plan: DecodePlan, k
             A.acache_argmax_commit(logits, out=pick, conf=conf, stream=stream)
             A.acache_threshold_commit(blen, pick, conf, tau, flags, plan.pos[blk], batch.remap, count,
                                       stream=stream)
-            with _on(stream):
-                count_host.copy_(count, non_blocking=True)
-            (stream if stream is not None else torch.cuda.current_stream()).synchronize()
+            count_host.copy_(count, non_blocking=True)
+            torch.cuda.current_stream().synchronize()
             if trace is not None:
                 trace.append(dict(block=blk, logits=logits.float().cpu().numpy(), pick=pick.cpu().numpy(),
                                   conf=conf.cpu().numpy(), committed=flags.cpu().numpy()))
