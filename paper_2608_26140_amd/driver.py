@@ -284,12 +284,30 @@ class AffixBatch:
         """Materialise the shared affix cache once (Sections 3.3, 4.2): a full
         forward of a donor sequence whose affix rows write to the shared slots.
         donor_x [n, d] layer-0 inputs (consumed), donor_pos / write_slots [n],
-        read_slots [n_keys] (the donor's logical view)."""
+        read_slots [n_keys] (the donor's logical view).  8-bit caches: an
+        affix written whole shares no scale with the one it replaces, nor do
+        the donor's other rows with what their slots' blocks held."""
         n = donor_x.shape[0]
+        if self.quant_block:
+            self._empty_replaced(write_slots)
         for i in range(self.model.n_layers):
             self.recompute_layer(i, [0, n], [0, read_slots.numel()], donor_x, donor_pos, write_slots, read_slots,
                                  stream=stream)
         return donor_x
+
+    def _empty_replaced(self, write_slots: torch.Tensor):
+        """Empties the blocks whose earlier entries end with these rows: an
+        affix block all of whose affix slots are written (the store itself
+        sees to whole blocks; the last one has slots that nothing is ever
+        written to), and a private block any slot of which is."""
+        n_blocks = self.scales.shape[2]
+        ok = (write_slots >= 0) & (write_slots < self.n_slots)
+        written = torch.zeros(n_blocks * self.quant_block + 1, dtype=torch.bool, device=self.device)
+        written[torch.where(ok, write_slots, n_blocks * self.quant_block).long()] = True
+        written[self.L:self.first_private * self.quant_block] = True
+        written = written[:-1].view(n_blocks, self.quant_block)
+        replaced = torch.cat([written[:self.first_private].all(1), written[self.first_private:].any(1)])
+        self.scales.masked_fill_(replaced[:, None], 0.0)
 
     @_on_its_stream
     def shift_affix(self, delta: int, stream=None):

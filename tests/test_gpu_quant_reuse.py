@@ -123,3 +123,45 @@ def test_captured_without_a_run_before():
         torch.cuda.synchronize()
         equal(out, want)
         equal(run(), want)
+
+
+@pytest.mark.parametrize("name,qb,paged", PLANS)
+def test_affix_materialised_anew(name, qb, paged):
+    """A second affix in the slots of a first, larger one; the donor's other
+    rows in slots of large rows."""
+    w = W.get_config(name)
+    fresh, used = (WL.build(w, quant_block=qb, block_size=paged).batch for _ in range(2))
+    occupy(used, np.arange(used.n_slots))
+    S, L, ab = fresh.S, fresh.L, fresh.ab
+    got = []
+    for b in (fresh, used):
+        slots = np.empty(S, dtype=np.int64)
+        inside = (np.arange(S) >= ab) & (np.arange(S) < ab + L)
+        slots[inside] = b.affix_slots.cpu().numpy()
+        slots[~inside] = b.private_slots(S - L)[-1]
+        slots = up_i32(slots)
+        g = torch.Generator(device="cuda").manual_seed(4)
+        x = torch.randn(S, w.dims.d_model, generator=g, device="cuda").to(torch.bfloat16)
+        b.materialize_affix(x, up_i32(np.arange(S)), slots, slots)
+        got.append([x, *(t for c in b.caches for t in A.acache_quant_load(b.model.dims, c, b.affix_slots))])
+    equal(got[1], got[0])
+    equal(chain(used, w), chain(fresh, w))
+
+
+def test_affix_materialised_in_parts():
+    """A call that writes some of the affix's rows keeps the others."""
+    w = W.get_config("mini-stack")
+    batch = WL.build(w, quant_block=64).batch
+    dims, c = batch.model.dims, batch.caches[0]
+    kept = batch.affix_slots[:-10].contiguous()
+    before = A.acache_quant_load(dims, c, kept)
+    x = torch.randn(10, w.dims.d_model, device="cuda").to(torch.bfloat16)
+    # write slots outside the cache are skipped, here as in every call
+    slots = torch.cat([batch.affix_slots[-8:], up_i32([-1, batch.n_slots])])
+    batch.materialize_affix(x, up_i32(np.arange(batch.L - 10, batch.L)), slots, batch.affix_slots)
+    after = A.acache_quant_load(dims, c, kept)
+    for a, b, s in zip(before, after, (c.k_scales, c.v_scales)):
+        step = s[kept.long() // 64].repeat_interleave(dims.head_dim, 1)
+        # at most rounded to the scale that the new rows need: half a step of e4m3 each
+        assert ((a.float() - b.float()).abs() <= torch.maximum(2.0 ** -4 * a.float().abs(), 2.0 ** -10 * step)).all()
+        assert b[-2:].any()
