@@ -312,16 +312,24 @@ class AffixBatch:
     @_on_its_stream
     def shift_affix(self, delta: int, stream=None):
         """Reuse the shared affix cache delta positions from where it was
-        materialised: its K rows are re-rotated in place at every layer (8-bit
-        caches: read back, turned and stored again)."""
+        materialised: its K rows are re-rotated in place at every layer.
+        8-bit caches: K is read back, turned and stored again, and each shift
+        rounds it anew (to bf16, then half a step of e4m3: up to 2^-4 of an
+        entry), so its error grows with the number of shifts and a shift by
+        -delta does not restore it: materialise the affix again rather than
+        shift it often.  V keeps its values."""
         slots = self.affix_slots
         d = torch.full((self.L,), int(delta), dtype=torch.int32, device=self.device)
-        rows = torch.arange(self.L, dtype=torch.int32, device=self.device)
+        if self.quant_block:
+            rows = torch.arange(self.L, dtype=torch.int32, device=self.device)
+            # the short last block, which no store writes whole: its scale, too, is that of the turned rows
+            short = slice(self.L // self.quant_block * self.quant_block, self.first_private * self.quant_block)
         for c in self.caches:
             k, v = (torch.empty((self.L, self.model.kv_width), dtype=self.model.dtype, device=self.device)
                     for _ in range(2))
             A.acache_quant_load(self.model.dims, c, slots, k, v, stream=stream)
             A.acache_rerotate_k(self.model.dims, k, rows, k, rows, d, stream=stream)
+            c.clear(short, stream=stream)
             A.acache_quant_store(self.model.dims, c, k, v, slots, ws=self.ws, stream=stream)
         for k in self.k_pools:
             A.acache_rerotate_k(self.model.dims, k, slots, k, slots, d, stream=stream)
