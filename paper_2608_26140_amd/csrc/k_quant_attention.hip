@@ -442,6 +442,15 @@ constexpr int kNwCopies = kNwTileB / 1024;
 constexpr int kNwWaveB = 2 * kNwTileB + 4 * kAuxB;  // a wave's LDS
 static_assert(kNwWaves * kNwWaveB >= 2 * 66 * 64 * 4, "room for two waves' results");
 
+// Between LDS writes of a wave's lanes and reads of what other lanes wrote, and
+// between such reads and the next writes: the LDS keeps a wave's order by
+// itself (nothing is waited for), and this makes the compiler keep it, which
+// sees one lane's addresses only.
+__device__ __forceinline__ void lane_handoff() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
 __device__ __forceinline__ int k_swizzle(int r) { return (r & 3) | ((r >> 1) & 4); }
 __device__ __forceinline__ bf16x8 v_fragment(const char* lds) {
   typedef int v2i32 __attribute__((__vector_size__(2 * sizeof(int))));
@@ -512,7 +521,7 @@ __global__ __launch_bounds__(64 * kNwWaves, 2) void quant_attention_narrow_kerne
     x.v = __builtin_amdgcn_raw_buffer_load_b32(vsres, off, 0, 0);
   };
   auto put_scales = [&](const Scales& x) {
-    *reinterpret_cast<uint32_t*>(k_scales + lane * 4) = x.k;
+    *reinterpret_cast<float*>(k_scales + lane * 4) = __uint_as_float(x.k);  // its readers' type
     *reinterpret_cast<float*>(v_scales + lane * 4) = pow2_below(__uint_as_float(x.v));
     return __builtin_amdgcn_ballot_w64(!(__uint_as_float(x.k) > 0.f) || !(__uint_as_float(x.v) > 0.f)) != 0;
   };
@@ -532,6 +541,7 @@ __global__ __launch_bounds__(64 * kNwWaves, 2) void quant_attention_narrow_kerne
   };
   auto put_codes = [&](int t, Codes& x, bool empty) {
     if (empty) {  // an empty block's codes stand for zeros
+      lane_handoff();
 #pragma unroll
       for (int i = 0; i < kNwCopies; ++i) {
         const int at = ((t & 1) * kNwTileK + 8 * i + lrow) * 4;
@@ -543,6 +553,7 @@ __global__ __launch_bounds__(64 * kNwWaves, 2) void quant_attention_narrow_kerne
           x.v[i][j] = ve ? x.v[i][j] : 0u;
         }
       }
+      lane_handoff();
     }
 #pragma unroll
     for (int i = 0; i < kNwCopies; ++i) {
@@ -628,20 +639,25 @@ __global__ __launch_bounds__(64 * kNwWaves, 2) void quant_attention_narrow_kerne
     const int s0 = load_slot(0), s1 = load_slot(1);
     int next = load_slot(2);
     put_offset(0, s0);
+    put_offset(1, s1);
+    lane_handoff();
     load_codes(0, x0);
     load_codes(1, x1);
     load_scales(0, s0, sa);
-    put_offset(1, s1);
     load_scales(1, s1, sb);
     for (int t = 0; t < n_t; t += 2) {
       const int u = t >> 1;
+      lane_handoff();
       const bool empty = put_scales(sa);
       put_codes(t, x0, empty);
+      lane_handoff();
       load_codes(t + 2, x0);
       step(t);
+      lane_handoff();
       put_codes(t + 1, x1, empty);
-      load_codes(t + 3, x1);
       put_offset(u + 2, next);  // over group u's
+      lane_handoff();
+      load_codes(t + 3, x1);
       sa = sb;
       load_scales(u + 2, next, sb);
       next = load_slot(u + 3);
