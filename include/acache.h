@@ -539,6 +539,16 @@ acache_status acache_quant_attention(const acache_dims* dims, const acache_ragge
                                      const int32_t* read_slots, const acache_quant_pool* pool, void* out, float* lse,
                                      void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* What acache_quant_attention launches for this batch and workspace: query
+ * tiles of a KV head (the query heads that share it are further queries) of the
+ * 256-query kernel and of the 32-query kernel, one of them 0 unless the latter
+ * takes what is left of a request behind its whole 256-query tiles, which it
+ * does where that is at most *rest queries; and the key splits.  No rows: no
+ * tiles.  Host arithmetic only. */
+acache_status acache_quant_attention_schedule(const acache_dims* dims, const acache_ragged* rg, size_t ws_bytes,
+                                              int32_t* wide_tiles, int32_t* narrow_tiles, int32_t* rest,
+                                              int32_t* splits);
+
 /* Workspace bytes for acache_quant_store into `pool` and for
  * acache_quant_attention of up to max_rows rows over it.  Returns 0 for
  * invalid dims or an invalid pool (its pointers are not looked at). */

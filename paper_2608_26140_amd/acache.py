@@ -106,6 +106,7 @@ def _load():
         "acache_quant_store": [ctypes.POINTER(Dims), QP, P, P, I64, I32, P, P, SZ, P],
         "acache_quant_load": [ctypes.POINTER(Dims), QP, P, I32, P, P, I64, P],
         "acache_quant_attention": [ctypes.POINTER(Dims), ctypes.POINTER(Ragged), P, P, QP, P, P, P, SZ, P],
+        "acache_quant_attention_schedule": [ctypes.POINTER(Dims), ctypes.POINTER(Ragged), SZ, PI, PI, PI, PI],
         "acache_quant_layer_recompute": [ctypes.POINTER(Dims), ctypes.POINTER(LayerWeights), ctypes.POINTER(Ragged),
                                          P, P, P, P, QP, ctypes.POINTER(ScoreArgs), P, SZ, P],
     })
@@ -675,6 +676,15 @@ def acache_quant_attention(dims: Dims, cu_rows, cu_keys, q: torch.Tensor, read_s
         ctypes.byref(dims), ctypes.byref(rg), q.data_ptr(), read_slots.data_ptr(), pool.ref, out.data_ptr(),
         _ptr(lse), _ptr(ws), 0 if ws is None else ws.nbytes, _stream(stream)))
     return out
+
+
+def acache_quant_attention_schedule(dims: Dims, cu_rows, cu_keys, ws_bytes: int = 0):
+    """(wide_tiles, narrow_tiles, rest, splits) acache_quant_attention takes."""
+    rg, keep = _ragged(cu_rows, cu_keys)
+    out = [ctypes.c_int32(0) for _ in range(4)]
+    _check("acache_quant_attention_schedule", lib.acache_quant_attention_schedule(
+        ctypes.byref(dims), ctypes.byref(rg), ws_bytes, *(ctypes.byref(o) for o in out)))
+    return tuple(o.value for o in out)
 
 
 def acache_quant_layer_workspace_size(dims: Dims, max_rows: int, batch: int, affix_len: int, pool: QuantPool) -> int:

@@ -1024,6 +1024,26 @@ acache_status acache_quant_attention(const acache_dims* dims, const acache_ragge
   return ACACHE_OK;
 }
 
+acache_status acache_quant_attention_schedule(const acache_dims* dims, const acache_ragged* rg, size_t ws_bytes,
+                                              int32_t* wide_tiles, int32_t* narrow_tiles, int32_t* rest,
+                                              int32_t* splits) {
+  acache_status st = check_dims(dims);
+  if (st != ACACHE_OK) return st;
+  CHECK(dims->dtype == ACACHE_BF16, ACACHE_ERR_UNSUPPORTED);
+  CHECK(wide_tiles && narrow_tiles && rest && splits, ACACHE_ERR_NULL);
+  Ragged r;
+  st = make_ragged(rg, r);
+  if (st != ACACHE_OK) return st;
+  st = check_quant_ragged(r, dims->n_heads);
+  if (st != ACACHE_OK) return st;
+  const QuantAttentionPlan plan = plan_quant_attention(r, dims->n_heads, dims->n_kv_heads, ws_bytes);
+  *wide_tiles = plan.wide_tiles;
+  *narrow_tiles = plan.narrow_tiles;
+  *rest = plan.rest;
+  *splits = plan.splits;
+  return ACACHE_OK;
+}
+
 // The 8-bit layer's workspace: a layer's, then the fresh K and V rows, the
 // indices 0, 1, .. that address them and the affix keys, those keys, and the
 // store's map.

@@ -163,6 +163,13 @@ hipError_t launch_iota(int32_t* out, int n, hipStream_t s);  // 0, 1, .., n - 1
 // part / part_bytes: optional space for key splits; quant_attention_part_bytes
 // of the most (row, head) pairs serves every smaller call.
 size_t quant_attention_part_bytes(int64_t pairs);
+// What a call takes: 256-query and 32-query tiles of a KV head (with both, the
+// latter are what is left of a request behind its whole 256-query tiles, where
+// that is at most `rest` queries), and key splits.
+struct QuantAttentionPlan {
+  int wide_tiles, narrow_tiles, rest, splits;
+};
+QuantAttentionPlan plan_quant_attention(const Ragged& rg, int H, int kv_heads, size_t part_bytes);
 hipError_t launch_quant_attention(const Ragged& rg, int H, const QuantPool& p, const void* q, const int32_t* read_slots,
                                   void* out, float* lse, float* part, size_t part_bytes, hipStream_t s);
 

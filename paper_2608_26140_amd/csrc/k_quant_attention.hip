@@ -804,10 +804,53 @@ Cost wide_cost(int64_t units, int n_kt, double memory_us, int64_t pairs, int64_t
 
 }  // namespace
 
+QuantAttentionPlan plan_quant_attention(const Ragged& rg, int H, int kv_heads, size_t part_bytes) {
+  const int64_t pairs = (int64_t)rg.cu_rows[rg.batch] * H;
+  QuantAttentionPlan plan = {0, 0, 0, 1};
+  if (pairs == 0) return plan;
+  // query tiles of each kernel, and of the wide kernel with the narrow one
+  // behind it on what is left of a request behind its whole tiles, where that
+  // is at most kRest[i] queries
+  constexpr int kRest[3] = {64, 128, kWdTileQ - 1};
+  int64_t narrow = 0, wide = 0, both_wide[3] = {}, both_narrow[3] = {};
+  int n_kt = 0;
+  double memory_us = 0.0;
+  for (int b = 0; b < rg.batch; ++b) {
+    const int64_t n = (int64_t)(rg.cu_rows[b + 1] - rg.cu_rows[b]) * (H / kv_heads);
+    narrow += (n + 31) / 32;
+    wide += (n + kWdTileQ - 1) / kWdTileQ;
+    for (int i = 0; i < 3; ++i) {
+      const bool few = n % kWdTileQ <= kRest[i];
+      both_wide[i] += few ? n / kWdTileQ : (n + kWdTileQ - 1) / kWdTileQ;
+      both_narrow[i] += few ? (n % kWdTileQ + 31) / 32 : 0;
+    }
+    n_kt = std::max(n_kt, (rg.cu_keys[b + 1] - rg.cu_keys[b] + kTileK - 1) / kTileK);
+    if (n > 0) memory_us += (rg.cu_keys[b + 1] - rg.cu_keys[b]) * (2.0 * kDh / 4.9e6) * kv_heads;
+  }
+  const int64_t fit = std::max<int64_t>(1, (int64_t)(part_bytes / ((kDh + 2) * sizeof(float))) / pairs);
+  const Cost cn = narrow_cost(narrow * kv_heads, n_kt, memory_us, pairs, fit);
+  const Cost cw = wide_cost(wide * kv_heads, n_kt, memory_us, pairs, fit);
+  // the two launches write no partials: a merge would cover every row
+  double both_us = 1e30;
+  int both = 0;
+  for (int i = 0; i < 3; ++i) {
+    if (!both_wide[i] || !both_narrow[i]) continue;
+    const double us = wide_cost(both_wide[i] * kv_heads, n_kt, memory_us, pairs, 1).us +
+                      narrow_cost(both_narrow[i] * kv_heads, n_kt, 0.0, pairs, 1).us;
+    if (us < both_us) both_us = us, both = i;
+  }
+  if (both_us < std::min(cn.us, cw.us)) plan = {(int)both_wide[both], (int)both_narrow[both], kRest[both], 1};
+  else if (cw.us < cn.us) plan = {(int)wide, 0, 0, cw.splits};
+  else plan = {0, (int)narrow, 0, cn.splits};
+  return plan;
+}
+
 hipError_t launch_quant_attention(const Ragged& rg, int H, const QuantPool& p, const void* q, const int32_t* read_slots,
                                   void* out, float* lse, float* part, size_t part_bytes, hipStream_t s) {
-  const int64_t rows = rg.cu_rows[rg.batch];
-  if (rows == 0) return hipSuccess;
+  const int64_t pairs = (int64_t)rg.cu_rows[rg.batch] * H;
+  if (pairs == 0) return hipSuccess;
+  const QuantAttentionPlan plan = plan_quant_attention(rg, H, p.heads, part_bytes);
+  const int splits = plan.splits;
   QAttnArgs a;
   a.p = p;
   a.q = (const bf16*)q;
@@ -817,67 +860,30 @@ hipError_t launch_quant_attention(const Ragged& rg, int H, const QuantPool& p, c
   a.H = H;
   a.rep = H / p.heads;
   a.rg = rg;
-  const int64_t pairs = rows * H;
-  // query tiles of each kernel, and of the wide kernel with the narrow one
-  // behind it on what is left of a request behind its whole tiles, where that
-  // is at most kRest[i] queries
-  constexpr int kRest[3] = {64, 128, kWdTileQ - 1};
-  int64_t narrow = 0, wide = 0, both_wide[3] = {}, both_narrow[3] = {};
-  int n_kt = 0;
-  double memory_us = 0.0;
-  for (int b = 0; b < rg.batch; ++b) {
-    const int64_t n = (int64_t)(rg.cu_rows[b + 1] - rg.cu_rows[b]) * a.rep;
-    narrow += (n + 31) / 32;
-    wide += (n + kWdTileQ - 1) / kWdTileQ;
-    for (int i = 0; i < 3; ++i) {
-      const bool few = n % kWdTileQ <= kRest[i];
-      both_wide[i] += few ? n / kWdTileQ : (n + kWdTileQ - 1) / kWdTileQ;
-      both_narrow[i] += few ? (n % kWdTileQ + 31) / 32 : 0;
-    }
-    n_kt = std::max(n_kt, (rg.cu_keys[b + 1] - rg.cu_keys[b] + kTileK - 1) / kTileK);
-    if (n > 0) memory_us += (rg.cu_keys[b + 1] - rg.cu_keys[b]) * (2.0 * kDh / 4.9e6) * p.heads;
-  }
-  const int64_t fit = std::max<int64_t>(1, (int64_t)(part_bytes / ((kDh + 2) * sizeof(float))) / pairs);
-  const Cost cn = narrow_cost(narrow * p.heads, n_kt, memory_us, pairs, fit);
-  const Cost cw = wide_cost(wide * p.heads, n_kt, memory_us, pairs, fit);
-  // the two launches write no partials: a merge would cover every row
-  double both_us = 1e30;
-  int both = 0;
-  for (int i = 0; i < 3; ++i) {
-    if (!both_wide[i] || !both_narrow[i]) continue;
-    const double us = wide_cost(both_wide[i] * p.heads, n_kt, memory_us, pairs, 1).us +
-                      narrow_cost(both_narrow[i] * p.heads, n_kt, 0.0, pairs, 1).us;
-    if (us < both_us) both_us = us, both = i;
-  }
+  a.splits = splits;
+  a.part_o = part;
+  a.part_ml = part ? part + (size_t)splits * pairs * kDh : nullptr;
   // one launch over each request's queries: all of them, or those left to (or
   // by) the other kernel
-  auto launch = [&](bool is_wide, bool share, int splits) {
+  auto launch = [&](bool is_wide) {
+    const bool share = plan.wide_tiles && plan.narrow_tiles;
     const int tq = is_wide ? kWdTileQ : 32;
     int tiles = 0;
     for (int b = 0; b < rg.batch; ++b) {
       const int n = (rg.cu_rows[b + 1] - rg.cu_rows[b]) * a.rep;
-      const int cut = n % kWdTileQ <= kRest[both] ? n - n % kWdTileQ : n;
+      const int cut = n % kWdTileQ <= plan.rest ? n - n % kWdTileQ : n;
       a.rg.tile_start[b] = tiles;
       a.v_lo[b] = share && !is_wide ? cut : 0;
       a.v_hi[b] = share && is_wide ? cut : n;
       tiles += (a.v_hi[b] - a.v_lo[b] + tq - 1) / tq;
     }
     a.rg.tile_start[rg.batch] = tiles;
-    a.splits = splits;
-    a.part_o = part;
-    a.part_ml = part ? part + (size_t)splits * pairs * kDh : nullptr;
     const dim3 grid((unsigned)((int64_t)tiles * p.heads * splits));
     if (is_wide) hipLaunchKernelGGL(quant_attention_wide_kernel, grid, dim3(kWdThreads), 0, s, a);
     else hipLaunchKernelGGL(quant_attention_narrow_kernel, grid, dim3(64 * kNwWaves), 0, s, a);
   };
-  if (both_us < std::min(cn.us, cw.us)) {
-    launch(true, true, 1);
-    launch(false, true, 1);
-    return hipGetLastError();
-  }
-  const bool is_wide = cw.us < cn.us;
-  const int splits = is_wide ? cw.splits : cn.splits;
-  launch(is_wide, false, splits);
+  if (plan.wide_tiles) launch(true);
+  if (plan.narrow_tiles) launch(false);
   if (splits > 1)
     hipLaunchKernelGGL(quant_attention_merge_kernel, dim3((unsigned)((pairs + 3) / 4)), dim3(256), 0, s,
                        (const float*)a.part_o, (const float*)a.part_ml, splits, pairs, a.out, lse);
