@@ -481,14 +481,14 @@ acache_status acache_linear(const acache_dims* dims, const void* a, const void* 
  * value is its code times its block's scale.  Scales are powers of two, so
  * the product is exact in bf16 and fp32 (a scale that a caller wrote itself is
  * read as the power of two at or below it, of exponents -117 .. 119); a scale
- * of 0 marks an empty block, whose slots read as zeros whatever their codes.  A new cache is made by
- * setting both scale arrays to zero; the codes need no initial value.
- * Clearing a block's scales empties it again, which a caller does when it
- * gives the block's slots to another request (otherwise the block keeps the
- * larger scale of its earlier entries until all of its slots are written by
- * one call).  head_dim % 16 == 0; the 8-bit calls otherwise take the dims
- * that acache_attention takes (of them they read n_heads, n_kv_heads,
- * head_dim and dtype). */
+ * of 0 marks an empty block, whose slots read as zeros whatever their codes.  A
+ * new cache is made by setting both scale arrays to zero; the codes need no
+ * initial value.  Clearing a block's scales empties it again, which a caller
+ * does when it gives the block's slots to another request or prompt (otherwise
+ * the block keeps the larger scale of its earlier entries until all of its
+ * slots are written by one call).  head_dim % 16 == 0; the 8-bit calls
+ * otherwise take the dims that acache_attention takes (of them they read
+ * n_heads, n_kv_heads, head_dim and dtype). */
 typedef struct {
   void* k_codes;   /* [n_slots, ld] one byte each, a slot's row H_kv heads of head_dim (K after rotation) */
   void* v_codes;   /* [n_slots, ld] */
@@ -530,6 +530,8 @@ acache_status acache_quant_load(const acache_dims* dims, const acache_quant_pool
 /* acache_quant_attention — acache_attention over an 8-bit cache: the same
  * operation, layouts and ragged batch with K_j and V_j the cache's values
  * (a slot outside [0, n_slots) is a key and a value of zeros, as there).
+ * Logits, weights' sums and outputs are summed in fp32; a softmax weight is
+ * rounded to bf16 for its product with V, as there.
  * bf16 only (ACACHE_ERR_UNSUPPORTED otherwise), n_slots * ld < 2^31, at most
  * 2^28 rows times heads and 2^29 keys of a request.
  * ws is optional: with acache_quant_workspace_size(dims, rows, pool) bytes

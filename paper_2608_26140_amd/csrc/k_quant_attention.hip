@@ -15,7 +15,10 @@
 // is read as V^T through transposing LDS reads.  Softmax runs in base 2 with a
 // running maximum that moves only when exceeded by more than 2^8.  Logits,
 // weights' sum and output are held in fp32; a weight is rounded to bf16 for
-// the product with V, as in the bf16 attention.
+// the product with V, half a step of 2^-8 of it, as in the bf16 attention: the
+// fp32 product has a sixteenth of the bf16 one's rate.  Against 64 bits the
+// outputs are off by 0.0017 to 0.0022 (relative); by 0.0017 with fp32 weights,
+// which is the rounding of the bf16 output.
 //
 // With grouped heads the query heads of a KV head are further queries of the
 // same tile: a request's query v is row v mod rows of head g rep + v / rows.
@@ -154,7 +157,7 @@ __device__ __forceinline__ void write_query(const QAttnArgs& a, int64_t pair, in
 // them behind its products, so that K and V are converted once for all the
 // queries: eight conversions of each for a lane's 32 logits.  (Codes copied to
 // LDS first, three tiles ahead, with slots and scales in rings of their own:
-// 286 us where this takes 270, 6052 rows of 32 heads over 2432 keys.)
+// 286 us where this takes 270, 6044 rows of 32 heads over 2432 keys.)
 // The loop is software pipelined: iteration t forms S(t + 1) while it
 // exponentiates tile t's logits, then adds tile t's P V while it takes tile
 // t + 1's maxima, and converts K(t + 3) and V(t + 2); a barrier at every second
@@ -424,7 +427,9 @@ __global__ __launch_bounds__(kWdThreads, 1) void quant_attention_wide_kernel(QAt
 // held in the same order; V by a transposing read of bytes (in each 16-lane
 // group lane i points at key i / 2, dimensions 8 (i % 2) .. + 7 and receives
 // dimension i of the 8 keys), unscaled, the scale being a factor of the weight
-// instead.  16-byte chunk c of row r lies at c ^ k_swizzle(r) (K) and
+// instead (which below 2^-126, a small weight at one of the smallest scales, is a
+// subnormal bf16: the product takes it, off by at most 2^-134, so an output by
+// at most 448 * 2^-134 for each key).  16-byte chunk c of row r lies at c ^ k_swizzle(r) (K) and
 // c ^ (r & 7) (V).  Slots are read and offsets and scales made for 64 keys at a
 // time, one key a lane.
 // Measured: keys that one request alone reads at 5.1 TB/s, the rate of a large
@@ -765,8 +770,11 @@ namespace {
 // its first loads 6, 7.5 with two workgroups on a CU; a step of the narrow
 // kernel (32 keys a wave) 0.95, or 1.65 with two workgroups on a CU; a tile of
 // the wide kernel 1.9, one workgroup a CU; a merge 3.5 and its partials at 3
-// TB/s.  memory_us: the keys at 4.9 TB/s on all CUs, each request's read once;
-// below it more splits gain nothing.
+// TB/s.  memory_us: the keys at 4.9 TB/s on all CUs, each request's read once,
+// which is what keys of a request's own cost at least; keys that requests share
+// come from the caches after the first and cost less than it says (32 requests
+// over a shared affix of 8192 keys and 512 of their own: 465 us, where the call
+// takes 235): there the estimate can leave splits unused.
 // Both sides of the choice, in us, narrow and wide at their best splits:
 //   32 rows, 32 heads, 1536 keys  11.6 / 12.0;  717 rows  38 / 41
 //   8 x 512 rows, 32 heads, 2432 keys  273 / 168
