@@ -114,7 +114,7 @@ def stats(argv):
     st = _rows(os.path.join(run_dir, f"{name}_kernel_stats.csv"))
     bench = json.loads(open(bench_json).read().strip().splitlines()[-1])
     lines = [f"# rocprofv3 kernel statistics: {bench['config']['workload']} step", "",
-             "command (from the repository root on the GPU box):", f"  {cmd}", "",
+             "command (from the repository root):", f"  {cmd}", "",
              f"{'kernel':92s} {'calls':>6s} {'avg_us':>10s} {'min_us':>9s} {'max_us':>9s} {'total_ms':>9s} {'pct':>6s}"]
     for r in st:
         lines.append(f"{short(r['Name']):92s} {r['Calls']:>6s} {float(r['AverageNs']) / 1e3:10.2f} "
@@ -153,7 +153,7 @@ def stats(argv):
 def calls(argv):
     run_dir, name, title, n, out, cmd = argv[:6]
     n = int(n)
-    lines = [f"# rocprofv3 kernel statistics: {title}", "", "command (from the repository root on the GPU box):", f"  {cmd}", "",
+    lines = [f"# rocprofv3 kernel statistics: {title}", "", "command (from the repository root):", f"  {cmd}", "",
              f"{'kernel':92s} {'a call':>7s} {'avg_us':>9s} {'min_us':>9s} {'us a call':>10s}"]
     total = 0.0
     for r in _rows(os.path.join(run_dir, f"{name}_kernel_stats.csv")):
@@ -197,7 +197,7 @@ def mfma(argv):
         a[3] += c.get("SQ_VALU_MFMA_BUSY_CYCLES", 0.0)
         a[4] += c.get("SQ_INSTS_VALU_MFMA_MOPS_BF16", 0.0)
     lines = [f"# MFMA activity per kernel: {workload} step (rocprofv3 SQ_VALU_MFMA_BUSY_CYCLES, GRBM_GUI_ACTIVE,",
-             "# SQ_INSTS_VALU_MFMA_MOPS_BF16)", "", "command (from the repository root on the GPU box):", f"  {cmd}", "",
+             "# SQ_INSTS_VALU_MFMA_MOPS_BF16)", "", "command (from the repository root):", f"  {cmd}", "",
              f"Dispatches of the last {steps} step(s).  GRBM_GUI_ACTIVE per dispatch is summed over the {XCDS} XCDs:",
              f"divided by {XCDS} and by the dispatch's duration it gives the clock.  MFMA busy =",
              f"SQ_VALU_MFMA_BUSY_CYCLES / (GRBM_GUI_ACTIVE / {XCDS} x {SIMDS} SIMDs): the share of cycles in which a",
@@ -244,7 +244,7 @@ def traffic(argv):
         return tot / max(units, 1), units / steps
 
     lines = [f"# HBM traffic per launch: {workload} step (rocprofv3 FETCH_SIZE / WRITE_SIZE)", "",
-             "commands (from the repository root on the GPU box), one pass per counter (C = FETCH_SIZE, WRITE_SIZE):",
+             "commands (from the repository root), one pass per counter (C = FETCH_SIZE, WRITE_SIZE):",
              f"  {step_cmd}", f"  {copy_cmd}", "",
              f"calibration: gather_rows_kernel identity copy of {mib} MiB reads {read_b} B, writes {write_b} B per launch;",
              f"  FETCH_SIZE reads {copy_mean(cfetch):.0f} KiB -> read scale {rs:.4f}; "
