@@ -116,9 +116,9 @@ __device__ __forceinline__ float group_top(float m, uint32_t* red) {
 // own, which no stale entry can pretend.
 // Bound by HBM: 3 bytes an element of bf16.  Workgroups of neighbouring heads
 // are neighbours in the grid, so that whole rows are read and written together
-// (8192 rows of 32 heads of 128: 43 us, 4.7 TB/s, and 4.8 the map; with a head's
-// workgroups together 85 in all).  A small call is its chain of reads: slots,
-// rows and old scale, codes (32 rows of 32 heads: 7.7 us).
+// (8192 rows of 32 heads of 128, from cold caches: 43 us, 4.6 TB/s, and 4.8 the
+// map; with a head's workgroups together 85 in all).  A small call is its chain
+// of reads: slots, rows and old scale, codes (32 rows of 32 heads: 7.2 us).
 // ============================================================================
 constexpr int kSmallRows = 1024;
 
@@ -302,7 +302,7 @@ __global__ __launch_bounds__(kThreads) void quant_store_kernel(StoreArgs<T> a) {
 // ============================================================================
 // Load: value = code * scale, exact.  One thread per 16 codes of K or V, 16
 // bytes read and 32 written (bf16).  Bound by HBM: 8192 rows of 32 heads of 128
-// take 39 us, 5.2 TB/s.
+// take 44 us from cold caches, 4.6 TB/s.
 // ============================================================================
 template <typename T>
 __global__ __launch_bounds__(kThreads) void quant_load_kernel(const uint8_t* __restrict__ kc,
