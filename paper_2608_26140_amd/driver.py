@@ -299,14 +299,16 @@ class AffixBatch:
         """Empties the blocks whose earlier entries end with these rows: an
         affix block all of whose affix slots are written (the store itself
         sees to whole blocks; the last one has slots that nothing is ever
-        written to), and a private block any slot of which is."""
+        written to) and, beside a whole affix, a private block any slot of
+        which is.  Rows that are part of an affix leave the rest as it was."""
         n_blocks = self.scales.shape[2]
         ok = (write_slots >= 0) & (write_slots < self.n_slots)
         written = torch.zeros(n_blocks * self.quant_block + 1, dtype=torch.bool, device=self.device)
         written[torch.where(ok, write_slots, n_blocks * self.quant_block).long()] = True
+        whole = written[:self.L].all()
         written[self.L:self.first_private * self.quant_block] = True
         written = written[:-1].view(n_blocks, self.quant_block)
-        replaced = torch.cat([written[:self.first_private].all(1), written[self.first_private:].any(1)])
+        replaced = torch.cat([written[:self.first_private].all(1), written[self.first_private:].any(1) & whole])
         self.scales.masked_fill_(replaced[:, None], 0.0)
 
     @_on_its_stream

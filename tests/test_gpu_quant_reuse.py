@@ -165,3 +165,18 @@ def test_affix_materialised_in_parts():
         # at most rounded to the scale that the new rows need: half a step of e4m3 each
         assert ((a.float() - b.float()).abs() <= torch.maximum(2.0 ** -4 * a.float().abs(), 2.0 ** -10 * step)).all()
         assert b[-2:].any()
+
+
+def test_parts_keep_the_other_rows_of_their_blocks():
+    """Rows written part by part, some outside the affix: a part leaves what the
+    parts before it stored in the same private block."""
+    w = W.get_config("mini-stack")
+    batch = WL.build(w, quant_block=64).batch
+    dims, c = batch.model.dims, batch.caches[0]
+    own = up_i32(batch.private_slots(60)[1])
+    first, second = own[:25].contiguous(), torch.cat([own[25:], batch.affix_slots[:20]])
+    for slots in (first, second):
+        x = torch.randn(len(slots), w.dims.d_model, device="cuda").to(torch.bfloat16)
+        batch.materialize_affix(x, up_i32(np.arange(len(slots))), slots, batch.affix_slots)
+    k, v = A.acache_quant_load(dims, c, own)
+    assert k.any(1).all() and v.any(1).all()
