@@ -301,14 +301,17 @@ class AffixBatch:
         sees to whole blocks; the last one has slots that nothing is ever
         written to) and, beside a whole affix, a private block any slot of
         which is.  Rows that are part of an affix leave the rest as it was."""
-        n_blocks = self.scales.shape[2]
+        n_blocks, n_affix = self.scales.shape[2], self.first_private
         ok = (write_slots >= 0) & (write_slots < self.n_slots)
         written = torch.zeros(n_blocks * self.quant_block + 1, dtype=torch.bool, device=self.device)
-        written[torch.where(ok, write_slots, n_blocks * self.quant_block).long()] = True
-        whole = written[:self.L].all()
-        written[self.L:self.first_private * self.quant_block] = True
+        written.index_fill_(0, torch.where(ok, write_slots, n_blocks * self.quant_block).long(), True)
+        written[self.L:n_affix * self.quant_block] = True
         written = written[:-1].view(n_blocks, self.quant_block)
-        replaced = torch.cat([written[:self.first_private].all(1), written[self.first_private:].any(1) & whole])
+        affix = written[:n_affix].all(1)
+        # index 0 is filled if some block is not whole (no reduction over many
+        # rows: a captured one may clear its counters by a memset)
+        seen = torch.zeros(2, dtype=torch.bool, device=self.device).index_fill_(0, affix.long(), True)
+        replaced = torch.cat([affix, written[n_affix:].any(1) & ~seen[0]])
         self.scales.masked_fill_(replaced[:, None], 0.0)
 
     @_on_its_stream

@@ -180,3 +180,26 @@ def test_parts_keep_the_other_rows_of_their_blocks():
         batch.materialize_affix(x, up_i32(np.arange(len(slots))), slots, batch.affix_slots)
     k, v = A.acache_quant_load(dims, c, own)
     assert k.any(1).all() and v.any(1).all()
+
+
+def test_affix_materialised_in_a_graph():
+    """Captured and replayed over large earlier rows: the eager call's bits."""
+    w = W.get_config("mini-stack")
+    batch = WL.build(w, quant_block=64).batch
+    g = torch.Generator(device="cuda").manual_seed(4)
+    rows = torch.randn(batch.L, w.dims.d_model, generator=g, device="cuda").to(torch.bfloat16)
+    x, pos = torch.empty_like(rows), up_i32(np.arange(batch.L))
+
+    def run():
+        x.copy_(rows)
+        batch.materialize_affix(x, pos, batch.affix_slots, batch.affix_slots)
+        return [x, *(t for c in batch.caches for t in A.acache_quant_load(batch.model.dims, c, batch.affix_slots))]
+    want = [t.clone() for t in run()]
+    graph, out = D.capture(run)
+    for _ in range(3):
+        occupy(batch, np.arange(batch.n_slots))
+        graph.replay()
+        torch.cuda.synchronize()
+        equal(out, want)
+        occupy(batch, np.arange(batch.n_slots))
+        equal(run(), want)
