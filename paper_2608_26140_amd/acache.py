@@ -150,6 +150,15 @@ def _stream(stream=None):
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
+_HERE = contextlib.nullcontext()
+
+
+def _own(stream):
+    """Tensors made inside belong to the stream that a call uses them on, and
+    torch's fills run on it."""
+    return _HERE if stream is None else torch.cuda.stream(stream)
+
+
 def _i32(values: Sequence[int]):
     arr = (ctypes.c_int32 * len(values))(*[int(v) for v in values])
     return arr
@@ -200,7 +209,8 @@ def acache_topk(scores: torch.Tensor, k: int, out: Optional[torch.Tensor] = None
         raise TypeError("scores must be a contiguous float32 [batch, L] tensor")
     b, L = scores.shape
     if out is None:
-        out = torch.empty((b, k), dtype=torch.int32, device=scores.device)
+        with _own(stream):
+            out = torch.empty((b, k), dtype=torch.int32, device=scores.device)
     _check("acache_topk", lib.acache_topk(_ptr(scores), b, L, k, _ptr(out), _stream(stream)))
     return out
 
@@ -213,7 +223,8 @@ def acache_gather_rows(src: torch.Tensor, idx: torch.Tensor, remap: Optional[tor
     src2 = src.reshape(src.shape[0], -1)
     n = idx.numel()
     if out is None:
-        out = torch.empty((n,) + tuple(src.shape[1:]), dtype=src.dtype, device=src.device)
+        with _own(stream):
+            out = torch.empty((n,) + tuple(src.shape[1:]), dtype=src.dtype, device=src.device)
     row_bytes = src2.shape[1] * src2.element_size()
     _check("acache_gather_rows", lib.acache_gather_rows(
         _ptr(src2), src2.stride(0) * src2.element_size(), src2.shape[0], _ptr(idx), _ptr(remap),
@@ -238,8 +249,9 @@ def acache_build_maps(layout: Layout, batch: int, anchors: Optional[torch.Tensor
         _dev_i32(anchors, "anchors")
     R = k + layout.seq_len - layout.affix_len
     t = lambda n: torch.empty(n, dtype=torch.int32, device=device)
-    out = dict(row_pos=t(batch * R), row_src=t(batch * R), write_slots=t(batch * R),
-               read_slots=t(batch * layout.seq_len), q_rows=t(batch * layout.mask_len))
+    with _own(stream):
+        out = dict(row_pos=t(batch * R), row_src=t(batch * R), write_slots=t(batch * R),
+                   read_slots=t(batch * layout.seq_len), q_rows=t(batch * layout.mask_len))
     _check("acache_build_maps", lib.acache_build_maps(
         ctypes.byref(layout), batch, _ptr(anchors) if k > 0 else None, k, _ptr(out["row_pos"]),
         _ptr(out["row_src"]), _ptr(out["write_slots"]), _ptr(out["read_slots"]), _ptr(out["q_rows"]),
@@ -258,8 +270,9 @@ def acache_build_maps_paged(layout: Layout, batch: int, anchors: Optional[torch.
             _dev_i32(t, n)
     R = k + layout.seq_len - layout.affix_len
     t = lambda n: torch.empty(n, dtype=torch.int32, device=device)
-    out = dict(row_pos=t(batch * R), row_src=t(batch * R), write_slots=t(batch * R),
-               read_slots=t(batch * layout.seq_len), q_rows=t(batch * layout.mask_len))
+    with _own(stream):
+        out = dict(row_pos=t(batch * R), row_src=t(batch * R), write_slots=t(batch * R),
+                   read_slots=t(batch * layout.seq_len), q_rows=t(batch * layout.mask_len))
     pg = Paging(block_size, blocks_per_request, None if shared_blocks is None else shared_blocks.data_ptr(),
                 None if private_blocks is None else private_blocks.data_ptr())
     _check("acache_build_maps_paged", lib.acache_build_maps_paged(
@@ -319,7 +332,8 @@ def acache_attention(dims: Dims, cu_rows, cu_keys, q: torch.Tensor, read_slots: 
     _dev_i32(read_slots, "read_slots")
     rg, keep = _ragged(cu_rows, cu_keys)
     if out is None:
-        out = torch.empty_like(q)
+        with _own(stream):
+            out = torch.empty_like(q)
     _check("acache_attention", lib.acache_attention(
         ctypes.byref(dims), ctypes.byref(rg), _ptr(q), _ptr(read_slots), _ptr(k_pool), _ptr(v_pool),
         k_pool.stride(0), k_pool.shape[0], _ptr(out), _ptr(lse), _stream(stream)))
@@ -431,7 +445,8 @@ def acache_layer_decode(dims: Dims, weights, batch: int, rows_per_request: int, 
 
 def acache_rmsnorm(dims: Dims, x: torch.Tensor, g: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None):
     if out is None:
-        out = torch.empty_like(x)
+        with _own(stream):
+            out = torch.empty_like(x)
     _check("acache_rmsnorm", lib.acache_rmsnorm(ctypes.byref(dims), _ptr(x), _ptr(g), _ptr(out), x.shape[0],
                                                 _stream(stream)))
     return out
@@ -444,7 +459,8 @@ def acache_linear(dims: Dims, a: torch.Tensor, w: torch.Tensor, out: Optional[to
     M, K = a.shape
     N = w.shape[0]
     if out is None:
-        out = torch.empty((M, N), dtype=a.dtype, device=a.device)
+        with _own(stream):
+            out = torch.empty((M, N), dtype=a.dtype, device=a.device)
     _check("acache_linear", lib.acache_linear(ctypes.byref(dims), _ptr(a), _ptr(w), _ptr(out), M, N, K,
                                               int(accumulate), _ptr(ws), 0 if ws is None else ws.numel(),
                                               _stream(stream)))
@@ -458,7 +474,8 @@ def acache_kv_deviation(dims: Dims, k_pool: torch.Tensor, v_pool: torch.Tensor, 
     assert fresh_slots.dtype == torch.int32 and fresh_slots.stride(1) == 1
     _dev_i32(stale_slots, "stale_slots")
     if scores is None:
-        scores = torch.empty((B, L), dtype=torch.float32, device=k_pool.device)
+        with _own(stream):
+            scores = torch.empty((B, L), dtype=torch.float32, device=k_pool.device)
     _check("acache_kv_deviation", lib.acache_kv_deviation(
         ctypes.byref(dims), B, L, _ptr(k_pool), _ptr(v_pool), k_pool.stride(0), k_pool.shape[0],
         _ptr(fresh_slots), fresh_slots.stride(0), _ptr(stale_slots), _ptr(scores), _stream(stream)))
@@ -484,7 +501,8 @@ def acache_argmax_commit(x: torch.Tensor, out: Optional[torch.Tensor] = None,
     optional) receives each row's largest softmax probability."""
     rows, n = x.shape
     if out is None:
-        out = torch.empty(rows, dtype=torch.int32, device=x.device)
+        with _own(stream):
+            out = torch.empty(rows, dtype=torch.int32, device=x.device)
     if commit_pos is not None:
         _dev_i32(commit_pos, "commit_pos")
         _dev_i32(ids, "ids")
@@ -583,15 +601,6 @@ def quant_workspace(dims: Dims, max_rows: int, pool: QuantPool) -> torch.Tensor:
     """Workspace for acache_quant_store into `pool` and acache_quant_attention
     of up to max_rows rows over it."""
     return torch.empty(acache_quant_workspace_size(dims, max_rows, pool), dtype=torch.uint8, device=pool.device)
-
-
-_HERE = contextlib.nullcontext()
-
-
-def _own(stream):
-    """Tensors made inside belong to the stream that a call uses them on, and
-    torch's fills run on it."""
-    return _HERE if stream is None else torch.cuda.stream(stream)
 
 
 def _quant_check(dims: Dims, pool: QuantPool, *tensors):
