@@ -580,6 +580,111 @@ size_t acache_quant_layer_workspace_size(const acache_dims* dims, int32_t max_ro
                                          const acache_quant_pool* pool);
 
 /* ---------------------------------------------------------------------------
+ * A cache in blocks with a table for each request (the private block tables of
+ * a paged slot plan, Section 4.1, or any other), for steps that name cache
+ * entries by a request's positions rather than by slot lists.  Position p of
+ * request b is slot tables[b * table_ld + p / block] * block + p % block of the
+ * pools.  A position that is negative or past the table, or whose entry is
+ * outside [0, n_blocks), has no slot: nothing is stored there and it reads as a
+ * key and a value of zeros.  Several requests may name one block (a shared
+ * prefix).  Slots are addressed with 64-bit offsets. */
+typedef struct {
+  void* k;               /* [n_blocks * block, ld] of dims->dtype, a slot's row H_kv heads of head_dim (K after rotation) */
+  void* v;
+  int64_t ld;            /* >= H_kv * head_dim */
+  int64_t n_blocks;      /* >= 1; n_blocks * block < 2^31 */
+  const int32_t* tables; /* [batch, table_ld] block ids; entries that hold no attended position are not read */
+  int64_t table_ld;      /* >= max_blocks */
+  int32_t batch;
+  int32_t max_blocks;    /* entries of a request's table; max_blocks * block < 2^31 */
+  int32_t block;         /* slots of a block, >= 1 */
+} acache_paged_cache;
+
+/* acache_paged_append — the store half of a step over such a cache, with the
+ * rotary embedding on the way: row m (request m / rows_per_request) of k is
+ * rotated on half-split pairs by pos[m] * theta_i, as acache_layer_recompute
+ * rotates, and goes with row m of v to the slot of position at[m] (at NULL:
+ * pos[m]).  With q (nullable) its rows are rotated likewise into q_out (which
+ * may be q itself).  A row with pos[m] < 0 is padding: nothing of it is stored
+ * and its row of q_out is zeros.  A row whose position has no slot is rotated
+ * but not stored.  Rows of one call name different slots (of two that name one,
+ * elements of either are stored).  Slots that no row names keep every bit.
+ *   q [rows, q_ld], q_out [rows, q_out_ld]: H * head_dim elements of a row
+ *   k [rows, k_ld], v [rows, v_ld]: H_kv * head_dim; rows = batch * rows_per_request
+ * A projection's fused rows serve as q, k and v with one stride.  The sources
+ * must not overlap the pools.  bf16: pointers and strides are multiples of 16
+ * bytes.  rows == 0: no-op. */
+acache_status acache_paged_append(const acache_dims* dims, const acache_paged_cache* cache, int32_t rows_per_request,
+                                  const void* q, int64_t q_ld, const void* k, int64_t k_ld, const void* v, int64_t v_ld,
+                                  const int32_t* pos, const int32_t* at, void* q_out, int64_t q_out_ld,
+                                  hipStream_t stream);
+
+/* acache_paged_attention — acache_attention of rows_per_request rows of each
+ * request over its positions: row m (request b = m / rows_per_request) attends
+ * to positions 0 .. key_len[m] - 1 (at most max_blocks * block of them; none if
+ * negative), so that a row's own length gives a new token, a block that sees
+ * its whole context, or causal rows:
+ *   out[m, h] = softmax_j(q[m, h] . K_j / sqrt(d_h)) V_j over those j,
+ * zeros for a row without keys (or whose logits are all -inf).  What the cache
+ * holds at positions that a row does not attend to, NaN and infinities
+ * included, does not reach it.  lse (nullable) [rows, H]: the natural-log
+ * log-sum-exp of the scaled logits, -inf for a row without keys.  Lengths and
+ * tables are read on the device, so a captured step follows them.
+ *   q [rows, q_ld], out [rows, out_ld]; bf16: pointers and strides are multiples
+ *   of 16 bytes, head_dim == 128; f32: head_dim <= 128.
+ * bf16 weights are rounded to bf16 for their product with V, as in
+ * acache_attention.  max_len [host]: about the longest key_len (<= 0: the
+ * tables' capacity); it sets how the keys are split over workgroups and nothing
+ * else.  ws is optional: with acache_paged_workspace_size() bytes calls with
+ * few rows split the keys (fp32 partials, joined in a fixed order); with less,
+ * in fewer parts or none.  rows == 0: no-op. */
+acache_status acache_paged_attention(const acache_dims* dims, const acache_paged_cache* cache, int32_t rows_per_request,
+                                     const void* q, int64_t q_ld, const int32_t* key_len, int64_t max_len, void* out,
+                                     int64_t out_ld, float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Workspace bytes with which acache_paged_attention splits the keys as it
+ * likes (its pointers are not looked at).  0 for invalid dims or cache, 256 at
+ * least otherwise. */
+size_t acache_paged_workspace_size(const acache_dims* dims, const acache_paged_cache* cache, int32_t rows_per_request,
+                                   int64_t max_len);
+
+/* The key splits acache_paged_attention takes with this workspace.  Host
+ * arithmetic only. */
+acache_status acache_paged_attention_schedule(const acache_dims* dims, const acache_paged_cache* cache,
+                                              int32_t rows_per_request, int64_t max_len, size_t ws_bytes, int32_t* splits);
+
+/* ---------------------------------------------------------------------------
+ * acache_sample_commit — acache_argmax_commit with a token drawn from each row
+ * by a given number instead of the largest.  The row's tokens are taken in
+ * order of their logits, largest first, equal ones (-0 == +0) by index, with
+ * weights exp((x - max) / temperature).  Of these are kept
+ *   - the first top_k (<= 0, or n and more: all);
+ *   - of those, the shortest run from the first whose weight is at least top_p
+ *     times theirs (top_p >= 1 or NaN: all; the first token is always kept);
+ *   - the ones with a weight of at least min_p times the largest (<= 0 or NaN:
+ *     all; above 1: as 1);
+ * and out[i] is the first token whose cumulative weight exceeds u times the
+ * weight of all kept.  u is taken within [0, 1] (NaN: 0); 64 bits of it, since
+ * with 24 a token of probability 2^-24 could not be told from its neighbours.
+ * A temperature that is not above 0 (NaN included) is greedy:
+ * acache_argmax_commit's token.  NaN and -inf weigh nothing; where a logit is
+ * +inf, only those do.  A row of neither gives acache_argmax_commit's token,
+ * with conf and prob 0.
+ *   temperature, top_p, min_p fp32, top_k int32: [rows], nullable (1; no cut)
+ *   u fp64 [rows]
+ *   conf (nullable) fp32 [rows]: the token's softmax probability at temperature
+ *     1 without cuts, what acache_threshold_commit compares
+ *   prob (nullable) fp32 [rows]: the probability it was drawn with (greedy: 1)
+ * commit_pos, ids: as in acache_argmax_commit.  Weights are summed as integers
+ * (2^-44 of the largest is 1), so the result does not depend on the order of
+ * the work.  n <= 2^19 (ACACHE_ERR_UNSUPPORTED otherwise).  rows == 0: no-op;
+ * n == 0 with rows > 0: ACACHE_ERR_SHAPE. */
+acache_status acache_sample_commit(acache_dtype dtype, const void* x, int64_t ld, int32_t rows, int32_t n,
+                                   const float* temperature, const int32_t* top_k, const float* top_p,
+                                   const float* min_p, const double* u, int32_t* out, float* conf, float* prob,
+                                   const int32_t* commit_pos, int32_t* ids, int64_t ids_len, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
  * Measurement hook (benchmarks only).  While armed for kernel `kernel`,
  * every launch of that kernel by any entry point records starts[i] before
  * and stops[i] after it on the launch stream, i = *count, *count + 1, ...,

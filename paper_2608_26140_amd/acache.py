@@ -61,6 +61,12 @@ class QuantPoolDesc(ctypes.Structure):
                 ("block", ctypes.c_int32)]
 
 
+class PagedCacheDesc(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("ld", ctypes.c_int64), ("n_blocks", ctypes.c_int64),
+                ("tables", ctypes.c_void_p), ("table_ld", ctypes.c_int64), ("batch", ctypes.c_int32),
+                ("max_blocks", ctypes.c_int32), ("block", ctypes.c_int32)]
+
+
 class Paging(ctypes.Structure):
     _fields_ = [("block_size", ctypes.c_int32), ("blocks_per_request", ctypes.c_int32),
                 ("shared_blocks", ctypes.c_void_p), ("private_blocks", ctypes.c_void_p)]
@@ -110,6 +116,13 @@ def _load():
         "acache_quant_layer_recompute": [ctypes.POINTER(Dims), ctypes.POINTER(LayerWeights), ctypes.POINTER(Ragged),
                                          P, P, P, P, QP, ctypes.POINTER(ScoreArgs), P, SZ, P],
     })
+    PC = ctypes.POINTER(PagedCacheDesc)
+    sig.update({
+        "acache_paged_append": [ctypes.POINTER(Dims), PC, I32, P, I64, P, I64, P, I64, P, P, P, I64, P],
+        "acache_paged_attention": [ctypes.POINTER(Dims), PC, I32, P, I64, P, I64, P, I64, P, P, SZ, P],
+        "acache_paged_attention_schedule": [ctypes.POINTER(Dims), PC, I32, I64, SZ, PI],
+        "acache_sample_commit": [I32, P, I64, I32, I32, P, P, P, P, P, P, P, P, P, P, I64, P],
+    })
     for name, args in sig.items():
         fn = getattr(lib, name)
         fn.argtypes = args
@@ -120,6 +133,8 @@ def _load():
     lib.acache_quant_workspace_size.restype = ctypes.c_size_t
     lib.acache_quant_layer_workspace_size.argtypes = [ctypes.POINTER(Dims), I32, I32, I32, QP]
     lib.acache_quant_layer_workspace_size.restype = ctypes.c_size_t
+    lib.acache_paged_workspace_size.argtypes = [ctypes.POINTER(Dims), PC, I32, I64]
+    lib.acache_paged_workspace_size.restype = ctypes.c_size_t
     lib.acache_status_string.argtypes = [ctypes.c_int32]
     lib.acache_status_string.restype = ctypes.c_char_p
     lib.acache_version.restype = ctypes.c_int32
@@ -733,6 +748,178 @@ def acache_quant_layer_recompute(dims: Dims, weights, cu_rows, cu_keys, x: torch
         ctypes.byref(dims), ctypes.byref(lw), ctypes.byref(rg), x.data_ptr(), pos.data_ptr(), write_slots.data_ptr(),
         read_slots.data_ptr(), pool.ref, ctypes.byref(sa) if sa is not None else None, ws.data_ptr(), ws.nbytes,
         _stream(stream)))
+
+
+# ---------------------------------------------------------------------------- a cache in blocks with tables
+class PagedCache:
+    """One layer's K and V pools [n_slots, >= n_kv_heads * head_dim] in blocks
+    of `block` consecutive slots, and a table of block ids for each request
+    (tables [batch, max_blocks] int32): position p of request b is slot
+    tables[b, p // block] * block + p % block.  Slots past the last whole
+    block belong to none.  The tables are read on the device by each call."""
+
+    def __init__(self, k_pool: torch.Tensor, v_pool: torch.Tensor, block: int, tables: torch.Tensor):
+        for t in (k_pool, v_pool):
+            if t.dtype not in (torch.bfloat16, torch.float32) or t.dim() != 2 or t.stride(1) != 1:
+                raise TypeError("pools must be bfloat16 or float32 [n_slots, ld] tensors with contiguous rows")
+        if k_pool.shape != v_pool.shape or k_pool.stride(0) != v_pool.stride(0) or k_pool.dtype != v_pool.dtype:
+            raise ValueError("k_pool and v_pool must have the same type, shape and row stride")
+        if tables.dtype != torch.int32 or tables.dim() != 2 or (tables.shape[1] > 1 and tables.stride(1) != 1):
+            raise TypeError("tables must be an int32 [batch, max_blocks] tensor with contiguous rows")
+        if block < 1 or k_pool.shape[0] < block:
+            raise ValueError("the pools must hold at least one block")
+        if any(t.device != k_pool.device for t in (v_pool, tables)):
+            raise ValueError("pools and tables must be on one device")
+        self.k_pool, self.v_pool, self.tables, self.block = k_pool, v_pool, tables, block
+        self.batch, self.max_blocks = tables.shape
+        self.width, self.device, self.dtype = k_pool.shape[1], k_pool.device, k_pool.dtype
+        # the stride of a single row says nothing
+        ld = k_pool.stride(0) if k_pool.shape[0] > 1 else self.width
+        table_ld = tables.stride(0) if self.batch > 1 else self.max_blocks
+        self.desc = PagedCacheDesc(k_pool.data_ptr(), v_pool.data_ptr(), ld, k_pool.shape[0] // block,
+                                   tables.data_ptr(), table_ld, self.batch, self.max_blocks, block)
+        self.ref = ctypes.byref(self.desc)
+
+
+def _paged_check(dims: Dims, cache: PagedCache, *tensors):
+    """The cache fits dims, and everything is on the current device."""
+    if cache.dtype != torch_dtype(dims) or cache.width < dims.n_kv_heads * dims.head_dim:
+        raise ValueError("the pools do not hold rows of dims.n_kv_heads heads of dims.head_dim of dims' type")
+    device = cache.device
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError(f"the cache is on {device}, not on the current device")
+    for t in tensors:
+        if t.device != device:
+            raise ValueError(f"a tensor is on {t.device} and the cache on {device}")
+
+
+def _row_ld(t: torch.Tensor, n: int, width: int, dt, name: str) -> int:
+    """The row stride of t: [n, width] of type dt, rows contiguous and apart."""
+    if t.dtype != dt or t.dim() != 2 or t.shape[0] != n or t.shape[1] != width or (width > 1 and t.stride(1) != 1):
+        raise TypeError(f"{name} must be a [{n}, {width}] {dt} tensor with contiguous rows")
+    return t.stride(0) if n > 1 else width
+
+
+def _dev_rows(t: torch.Tensor, n: int, dt, name: str):
+    if t.dtype != dt or not t.is_contiguous() or t.numel() != n:
+        raise TypeError(f"{name} must be a contiguous {dt} tensor of {n} values")
+
+
+def acache_paged_append(dims: Dims, cache: PagedCache, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor,
+                        rows_per_request: int, at: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
+                        q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """Rows of K, rotated at pos, and of V go to the slots of positions `at`
+    (None: pos) of their requests, rows_per_request rows each; q (optional) is
+    rotated into q_out, which is returned.  Row views of a fused projection
+    serve as q, k and v."""
+    n, hq, hkv = cache.batch * rows_per_request, dims.n_heads * dims.head_dim, dims.n_kv_heads * dims.head_dim
+    dt = torch_dtype(dims)
+    k_ld, v_ld = _row_ld(k, n, hkv, dt, "k"), _row_ld(v, n, hkv, dt, "v")
+    _dev_rows(pos, n, torch.int32, "pos")
+    if at is not None:
+        _dev_rows(at, n, torch.int32, "at")
+    if q is None and q_out is not None:
+        raise ValueError("q_out without q")
+    q_ld = q_out_ld = 0
+    if q is not None:
+        q_ld = _row_ld(q, n, hq, dt, "q")
+        if q_out is None:
+            with _own(stream):
+                q_out = torch.empty((n, hq), dtype=dt, device=q.device)
+        q_out_ld = _row_ld(q_out, n, hq, dt, "q_out")
+    _paged_check(dims, cache, *(t for t in (k, v, pos, at, q, q_out) if t is not None))
+    _check("acache_paged_append", lib.acache_paged_append(
+        ctypes.byref(dims), cache.ref, rows_per_request, _ptr(q), q_ld, k.data_ptr(), k_ld, v.data_ptr(), v_ld,
+        pos.data_ptr(), _ptr(at), _ptr(q_out), q_out_ld, _stream(stream)))
+    return q_out
+
+
+def acache_paged_workspace_size(dims: Dims, cache: PagedCache, rows_per_request: int, max_len: int = 0) -> int:
+    n = lib.acache_paged_workspace_size(ctypes.byref(dims), cache.ref, rows_per_request, max_len)
+    if n == 0:
+        raise AcacheError("acache_paged_workspace_size", 2, "invalid dims or cache")
+    return n
+
+
+def paged_workspace(dims: Dims, cache: PagedCache, rows_per_request: int, max_len: int = 0) -> torch.Tensor:
+    """Workspace for acache_paged_attention of rows_per_request rows of each
+    of the cache's requests."""
+    return torch.empty(acache_paged_workspace_size(dims, cache, rows_per_request, max_len), dtype=torch.uint8,
+                       device=cache.device)
+
+
+def acache_paged_attention(dims: Dims, cache: PagedCache, q: torch.Tensor, key_len: torch.Tensor,
+                           rows_per_request: int, max_len: int = 0, out: Optional[torch.Tensor] = None,
+                           lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                           stream=None) -> torch.Tensor:
+    """Row m of q [batch * rows_per_request, n_heads * head_dim] over the first
+    key_len[m] positions of its request.  ws (optional, from paged_workspace):
+    lets the keys of few rows be split over workgroups; max_len (optional):
+    about the longest of key_len, for that split."""
+    n, hq = cache.batch * rows_per_request, dims.n_heads * dims.head_dim
+    dt = torch_dtype(dims)
+    q_ld = _row_ld(q, n, hq, dt, "q")
+    _dev_rows(key_len, n, torch.int32, "key_len")
+    if out is None:
+        with _own(stream):
+            out = torch.empty((n, hq), dtype=dt, device=q.device)
+    out_ld = _row_ld(out, n, hq, dt, "out")
+    if lse is not None:
+        _dev_rows(lse, n * dims.n_heads, torch.float32, "lse")
+    _paged_check(dims, cache, *(t for t in (q, key_len, out, lse, ws) if t is not None))
+    _check("acache_paged_attention", lib.acache_paged_attention(
+        ctypes.byref(dims), cache.ref, rows_per_request, q.data_ptr(), q_ld, key_len.data_ptr(), max_len,
+        out.data_ptr(), out_ld, _ptr(lse), _ptr(ws), 0 if ws is None else ws.nbytes, _stream(stream)))
+    return out
+
+
+def acache_paged_attention_schedule(dims: Dims, cache: PagedCache, rows_per_request: int, max_len: int = 0,
+                                    ws_bytes: int = 0) -> int:
+    """The key splits acache_paged_attention takes with this workspace."""
+    out = ctypes.c_int32(0)
+    _check("acache_paged_attention_schedule", lib.acache_paged_attention_schedule(
+        ctypes.byref(dims), cache.ref, rows_per_request, max_len, ws_bytes, ctypes.byref(out)))
+    return out.value
+
+
+def acache_sample_commit(x: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Tensor] = None,
+                         top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+                         min_p: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                         conf: Optional[torch.Tensor] = None, prob: Optional[torch.Tensor] = None,
+                         commit_pos: Optional[torch.Tensor] = None, ids: Optional[torch.Tensor] = None,
+                         stream=None) -> torch.Tensor:
+    """A token of each row of logits x [rows, n], drawn by u (float64 [rows],
+    within [0, 1)) after temperature, top-k, top-p and min-p (each [rows],
+    optional); with commit_pos, also ids[commit_pos[i]] = row i's token.  conf
+    and prob (fp32 [rows], optional) receive its softmax probability and the
+    one it was drawn with (see the header)."""
+    if x.dim() != 2 or x.dtype not in (torch.bfloat16, torch.float32) or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise TypeError("x must be a bfloat16 or float32 [rows, n] tensor with contiguous rows")
+    rows, n = x.shape
+    _dev_rows(u, rows, torch.float64, "u")
+    f32 = torch.float32
+    for t, dt, name in ((temperature, f32, "temperature"), (top_k, torch.int32, "top_k"), (top_p, f32, "top_p"),
+                        (min_p, f32, "min_p"), (conf, f32, "conf"), (prob, f32, "prob"), (out, torch.int32, "out"),
+                        (commit_pos, torch.int32, "commit_pos")):
+        if t is not None:
+            _dev_rows(t, rows, dt, name)
+    if (commit_pos is None) != (ids is None):
+        raise ValueError("commit_pos and ids go together")
+    if ids is not None:
+        _dev_i32(ids, "ids")
+    if x.device.type != "cuda" or x.device.index != torch.cuda.current_device():
+        raise ValueError(f"x is on {x.device}, not on the current device")
+    if out is None:
+        with _own(stream):
+            out = torch.empty(rows, dtype=torch.int32, device=x.device)
+    for t in (u, temperature, top_k, top_p, min_p, out, conf, prob, commit_pos, ids):
+        if t is not None and t.device != x.device:
+            raise ValueError(f"a tensor is on {t.device} and x on {x.device}")
+    _check("acache_sample_commit", lib.acache_sample_commit(
+        ACACHE_BF16 if x.dtype == torch.bfloat16 else ACACHE_F32, x.data_ptr(), x.stride(0) if rows > 1 else n, rows, n,
+        _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), u.data_ptr(), out.data_ptr(), _ptr(conf), _ptr(prob),
+        _ptr(commit_pos), _ptr(ids), 0 if ids is None else ids.numel(), _stream(stream)))
+    return out
 
 
 # ---------------------------------------------------------------------------- measurement hook

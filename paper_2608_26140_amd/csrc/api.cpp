@@ -1151,4 +1151,117 @@ acache_status acache_quant_layer_recompute(const acache_dims* dims, const acache
   return run_out_mlp_bf16(dims, w, M, x, y, o, at<char>(ws, lp.h), part, stream);
 }
 
+// ---- a cache in blocks with tables
+namespace {
+
+acache_status check_paged(const acache_dims* d, const acache_paged_cache* c, int32_t rows_per_request, PagedCache& out) {
+  acache_status st = check_dims(d);
+  if (st != ACACHE_OK) return st;
+  CHECK(c, ACACHE_ERR_NULL);
+  CHECK(c->batch >= 0 && rows_per_request >= 0 && c->max_blocks >= 0 && c->n_blocks >= 0 && c->block >= 1,
+        ACACHE_ERR_SHAPE);
+  CHECK(c->table_ld >= c->max_blocks && c->ld >= (int64_t)d->n_kv_heads * d->head_dim, ACACHE_ERR_SHAPE);
+  constexpr int64_t k31 = (int64_t)1 << 31;
+  CHECK(c->n_blocks < k31 && c->n_blocks * c->block < k31 && (int64_t)c->max_blocks * c->block < k31,
+        ACACHE_ERR_UNSUPPORTED);
+  CHECK((int64_t)c->batch * rows_per_request < k31 / 2, ACACHE_ERR_UNSUPPORTED);
+  out = PagedCache{c->k, c->v, c->ld, (int)c->n_blocks, c->block, d->n_kv_heads, d->head_dim, c->tables, c->table_ld,
+                   c->batch, c->max_blocks};
+  return ACACHE_OK;
+}
+
+// Pools and a bf16 call's row buffers: 16-byte pieces.
+bool aligned_rows(const void* p, int64_t ld, int64_t es) { return aligned16(p) && ld * es % 16 == 0; }
+
+PagedPlan plan_paged(const acache_dims* d, const PagedCache& c, int32_t rows_per_request, int64_t max_len, size_t ws_bytes) {
+  const int64_t capacity = (int64_t)c.max_blocks * c.block;
+  return plan_paged_attention(d->dtype, c, rows_per_request, d->n_heads,
+                              max_len <= 0 ? capacity : std::min(max_len, capacity), ws_bytes);
+}
+
+}  // namespace
+
+acache_status acache_paged_append(const acache_dims* dims, const acache_paged_cache* cache, int32_t rows_per_request,
+                                  const void* q, int64_t q_ld, const void* k, int64_t k_ld, const void* v, int64_t v_ld,
+                                  const int32_t* pos, const int32_t* at, void* q_out, int64_t q_out_ld,
+                                  hipStream_t stream) {
+  PagedCache c;
+  acache_status st = check_paged(dims, cache, rows_per_request, c);
+  if (st != ACACHE_OK) return st;
+  const int64_t n = (int64_t)c.batch * rows_per_request;
+  if (n == 0) return ACACHE_OK;
+  CHECK(k && v && pos && (!q || q_out), ACACHE_ERR_NULL);
+  CHECK(c.k && c.v && (c.tables || c.max_blocks == 0), ACACHE_ERR_NULL);
+  CHECK(c.n_blocks > 0, ACACHE_ERR_SHAPE);
+  const int64_t hq = (int64_t)dims->n_heads * dims->head_dim, hkv = (int64_t)dims->n_kv_heads * dims->head_dim;
+  CHECK(k_ld >= hkv && v_ld >= hkv && (!q || (q_ld >= hq && q_out_ld >= hq)), ACACHE_ERR_SHAPE);
+  const int64_t es = (int64_t)elem_size(dims->dtype);
+  const bool rows16 = aligned_rows(c.k, c.ld, es) && aligned_rows(c.v, c.ld, es) && aligned_rows(k, k_ld, es) &&
+                      aligned_rows(v, v_ld, es) && (!q || (aligned_rows(q, q_ld, es) && aligned_rows(q_out, q_out_ld, es)));
+  CHECK(dims->dtype == ACACHE_F32 || rows16, ACACHE_ERR_ALIGN);
+  const AppendRows r = {q, k, v, q_out, q_ld, k_ld, v_ld, q_out_ld, pos, at, (int)n, rows_per_request, dims->n_heads,
+                        rows16 && dims->head_dim % 8 == 0};
+  LAUNCH_T(ACACHE_K_SCATTER, stream, launch_paged_append(dims->dtype, c, r, dims->rope_base, stream));
+  return ACACHE_OK;
+}
+
+acache_status acache_paged_attention(const acache_dims* dims, const acache_paged_cache* cache, int32_t rows_per_request,
+                                     const void* q, int64_t q_ld, const int32_t* key_len, int64_t max_len, void* out,
+                                     int64_t out_ld, float* lse, void* ws, size_t ws_bytes, hipStream_t stream) {
+  PagedCache c;
+  acache_status st = check_paged(dims, cache, rows_per_request, c);
+  if (st != ACACHE_OK) return st;
+  const int64_t n = (int64_t)c.batch * rows_per_request;
+  if (n == 0) return ACACHE_OK;
+  CHECK(q && key_len && out, ACACHE_ERR_NULL);
+  CHECK(c.k && c.v && (c.tables || c.max_blocks == 0), ACACHE_ERR_NULL);
+  CHECK(c.n_blocks > 0, ACACHE_ERR_SHAPE);
+  const int64_t hq = (int64_t)dims->n_heads * dims->head_dim;
+  CHECK(q_ld >= hq && out_ld >= hq, ACACHE_ERR_SHAPE);
+  if (dims->dtype == ACACHE_BF16)
+    CHECK(aligned_rows(c.k, c.ld, 2) && aligned_rows(c.v, c.ld, 2) && aligned_rows(q, q_ld, 2) && aligned_rows(out, out_ld, 2),
+          ACACHE_ERR_ALIGN);
+  CHECK(!ws || aligned16(ws), ACACHE_ERR_ALIGN);
+  const PagedPlan plan = plan_paged(dims, c, rows_per_request, max_len, ws ? ws_bytes : 0);
+  // one dimension of workgroups, of four (row, head) pairs each in the join
+  CHECK(((int64_t)c.batch * c.kv_heads * plan.splits + 8) * plan.tiles < (int64_t)1 << 31 && n * dims->n_heads < (int64_t)1 << 32,
+        ACACHE_ERR_UNSUPPORTED);
+  const PagedQueries r = {q, q_ld, out, out_ld, lse, key_len, rows_per_request, dims->n_heads};
+  LAUNCH_T(ACACHE_K_ATTENTION, stream, launch_paged_attention(dims->dtype, c, r, plan, ws, stream));
+  return ACACHE_OK;
+}
+
+size_t acache_paged_workspace_size(const acache_dims* dims, const acache_paged_cache* cache, int32_t rows_per_request,
+                                   int64_t max_len) {
+  PagedCache c;
+  if (check_paged(dims, cache, rows_per_request, c) != ACACHE_OK) return 0;
+  if (c.batch == 0 || rows_per_request == 0) return kAlign;
+  return std::max(kAlign, align_up(plan_paged(dims, c, rows_per_request, max_len, SIZE_MAX).ws_bytes));
+}
+
+acache_status acache_paged_attention_schedule(const acache_dims* dims, const acache_paged_cache* cache,
+                                              int32_t rows_per_request, int64_t max_len, size_t ws_bytes, int32_t* splits) {
+  PagedCache c;
+  acache_status st = check_paged(dims, cache, rows_per_request, c);
+  if (st != ACACHE_OK) return st;
+  CHECK(splits, ACACHE_ERR_NULL);
+  *splits = c.batch == 0 || rows_per_request == 0 ? 0 : plan_paged(dims, c, rows_per_request, max_len, ws_bytes).splits;
+  return ACACHE_OK;
+}
+
+acache_status acache_sample_commit(acache_dtype dtype, const void* x, int64_t ld, int32_t rows, int32_t n,
+                                   const float* temperature, const int32_t* top_k, const float* top_p,
+                                   const float* min_p, const double* u, int32_t* out, float* conf, float* prob,
+                                   const int32_t* commit_pos, int32_t* ids, int64_t ids_len, hipStream_t stream) {
+  CHECK(dtype == ACACHE_BF16 || dtype == ACACHE_F32, ACACHE_ERR_UNSUPPORTED);
+  CHECK(rows >= 0 && n >= 0 && ld >= n && ids_len >= 0, ACACHE_ERR_SHAPE);
+  if (rows == 0) return ACACHE_OK;
+  CHECK(n > 0, ACACHE_ERR_SHAPE);
+  CHECK(n <= 1 << 19, ACACHE_ERR_UNSUPPORTED);
+  CHECK(x && u && out && (!commit_pos || ids), ACACHE_ERR_NULL);
+  const SampleRows r = {x, ld, n, temperature, top_p, min_p, top_k, u, out, conf, prob, commit_pos, ids, ids_len};
+  LAUNCH_T(ACACHE_K_ARGMAX, stream, launch_sample_commit(dtype, r, rows, stream));
+  return ACACHE_OK;
+}
+
 }  // extern "C"

@@ -173,6 +173,63 @@ QuantAttentionPlan plan_quant_attention(const Ragged& rg, int H, int kv_heads, s
 hipError_t launch_quant_attention(const Ragged& rg, int H, const QuantPool& p, const void* q, const int32_t* read_slots,
                                   void* out, float* lse, float* part, size_t part_bytes, hipStream_t s);
 
+// ---- a cache in blocks with tables (k_paged.hip)
+struct PagedCache {
+  void* k;
+  void* v;
+  int64_t ld;
+  int n_blocks, block, kv_heads, head_dim;
+  const int32_t* tables;  // [batch, table_ld], max_blocks entries of a row
+  int64_t table_ld;
+  int batch, max_blocks;
+};
+struct AppendRows {  // rows [n, *_ld]; q (null: none) is written turned to q_out
+  const void *q, *k, *v;
+  void* q_out;
+  int64_t q_ld, k_ld, v_ld, q_out_ld;
+  const int32_t *pos, *at;  // at null: pos
+  int n, per_request, heads;
+  bool vec;  // fp32: head_dim, pointers and strides allow runs of four elements
+};
+hipError_t launch_paged_append(acache_dtype dt, const PagedCache& c, const AppendRows& r, float rope_base, hipStream_t s);
+struct PagedQueries {
+  const void* q;
+  int64_t q_ld;
+  void* out;
+  int64_t out_ld;
+  float* lse;  // nullable
+  const int32_t* key_len;
+  int per_request, heads;
+};
+// tile: queries of a KV head that a workgroup takes; splits: of the keys, their
+// partials in ws_bytes of workspace (part [splits][pairs][head_dim], stats).
+struct PagedPlan {
+  int tile, tiles, splits;
+  size_t ws_bytes;
+  float* part;
+  float2* stats;
+};
+PagedPlan plan_paged_attention(acache_dtype dt, const PagedCache& c, int per_request, int heads, int64_t max_len,
+                               size_t ws_bytes);
+hipError_t launch_paged_attention(acache_dtype dt, const PagedCache& c, const PagedQueries& r, const PagedPlan& plan,
+                                  void* ws, hipStream_t s);
+
+// ---- sampled commit (k_sample.hip); the settings are [rows] or null
+struct SampleRows {
+  const void* x;
+  int64_t ld;
+  int n;
+  const float *temperature, *top_p, *min_p;
+  const int32_t* top_k;
+  const double* u;
+  int32_t* out;
+  float *conf, *prob;  // nullable
+  const int32_t* commit_pos;
+  int32_t* ids;
+  int64_t ids_len;
+};
+hipError_t launch_sample_commit(acache_dtype dt, const SampleRows& r, int rows, hipStream_t s);
+
 // ---- fp32 path (k_f32.hip)
 hipError_t launch_gemm_f32(const float* X, const float* W, float* C, int64_t ldc, int M, int N,
                            int K, int accumulate, hipStream_t s);
