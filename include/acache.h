@@ -591,7 +591,7 @@ size_t acache_quant_layer_workspace_size(const acache_dims* dims, int32_t max_ro
 typedef struct {
   void* k;               /* [n_blocks * block, ld] of dims->dtype, a slot's row H_kv heads of head_dim (K after rotation) */
   void* v;
-  int64_t ld;            /* >= H_kv * head_dim */
+  int64_t ld;            /* >= H_kv * head_dim, < 2^30 */
   int64_t n_blocks;      /* >= 1; n_blocks * block < 2^31 */
   const int32_t* tables; /* [batch, table_ld] block ids; entries that hold no attended position are not read */
   int64_t table_ld;      /* >= max_blocks */

@@ -1162,6 +1162,7 @@ acache_status check_paged(const acache_dims* d, const acache_paged_cache* c, int
         ACACHE_ERR_SHAPE);
   CHECK(c->table_ld >= c->max_blocks && c->ld >= (int64_t)d->n_kv_heads * d->head_dim, ACACHE_ERR_SHAPE);
   constexpr int64_t k31 = (int64_t)1 << 31;
+  CHECK(c->ld < k31 / 2, ACACHE_ERR_UNSUPPORTED);
   CHECK(c->n_blocks < k31 && c->n_blocks * c->block < k31 && (int64_t)c->max_blocks * c->block < k31,
         ACACHE_ERR_UNSUPPORTED);
   CHECK((int64_t)c->batch * rows_per_request < k31 / 2, ACACHE_ERR_UNSUPPORTED);

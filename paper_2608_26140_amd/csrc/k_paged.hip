@@ -91,6 +91,8 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedCache c, AppendR
 }
 
 // ---------------------------------------------------------------- attention
+constexpr int kMaxSplits = 256;
+
 // Query p = i * rep + j of KV head g is row i of the request, head g * rep + j.
 struct Group {
   int b, g, split, tile;
@@ -131,27 +133,52 @@ __device__ __forceinline__ bool odd_word(uint32_t w) {
   return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u;
 }
 
+// The largest of a value in the four lanes lane % 16, + 16, + 32, + 48.
+__device__ __forceinline__ float most_of_four(float v) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
 // Attention of 16 QT queries of a KV head over a share of the keys.  Four
 // waves take 32 keys each at a time and keep their own running maximum, sum
 // and output; they meet at the end.  Nothing passes through LDS on the way:
 //  - S^T = K Q^T on MFMA 16x16x32: a lane's K fragment is 16 consecutive bytes
 //    of a key's row, straight from memory; the result leaves a lane four keys
 //    (4 (lane / 16) + j) of two 16-key tiles for query lane % 16, whose maxima
-//    need two exchanges between lanes;
+//    need two swaps between lanes;
 //  - O^T = V^T P^T: those eight keys, in that order, are the lane's B fragment
 //    (the order of the contraction is free), and for the A fragment a lane
 //    loads 16 bytes of each of the same eight keys' rows, elements 8 (lane %
 //    16) and on, and turns the 8 x 8 block in registers: row m of product i is
 //    element 8 m + i.
-// 16 KB are loaded a step and wave; eight waves a CU keep 128 KB in flight,
-// several times what the memory's latency asks for at a CU's share of its rate.
+// 16 KB are loaded a step and wave; two workgroups share a CU, and their eight
+// waves keep 128 KB in flight, several times what the memory's latency asks for
+// at a CU's share of its rate.  The block ids of the next step's keys are on
+// their way meanwhile.
+// The running maximum is raised only where the logits pass it by kSlack powers
+// of two (weights then reach 2^kSlack, which their types hold as well): with
+// random keys it rises for some query at almost every step, and each rise
+// scales the whole output.
 // A weight is rounded to bf16 for its product with V (2^-8 relative at most); its sum
 // is of the unrounded ones.
-template <int QT>
-__global__ __launch_bounds__(256) void paged_attention_kernel(PagedCache c, PagedQueries r, PagedPlan p) {
+constexpr float kSlack = 8.f;
+// RUNS: blocks are of whole runs of 16 slots, so that the 16 keys of a tile lie
+// one behind the other: their rows are a scalar base and per-lane offsets that
+// do not change.  Otherwise every lane finds the slot of one key and the others
+// get it from there (a third of the step's vector instructions).
+template <int QT, bool RUNS>
+__global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedCache c, PagedQueries r, PagedPlan p) {
   constexpr int LDO = 132;  // padded rows of the exchange
-  __shared__ float s_out[4][16][LDO];
-  __shared__ float s_m[4][16], s_l[4][16];
+  struct Mine {             // a wave's: the rows on their way, then its results
+    union {
+      char rows[2][8192];
+      float out[16 * QT][LDO];
+    };
+  };
+  __shared__ __attribute__((aligned(1024))) Mine s_mine[4];
+  __shared__ float s_m[4][16 * QT], s_l[4][16 * QT];
   Group gr;
   if (!group_of(c, p, gr)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -189,6 +216,7 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedCache c, Page
   const bf16* vp = (const bf16*)c.v + gr.g * 128;
   const float scale = kLog2e * 0.08838834764831845f;  // log2(e) / sqrt(128)
 
+  // m: of the logits as they come from the product; weights 2^(scale (s - m))
   float m[QT], l[QT];
   f32x4 acc[QT][8];
 #pragma unroll
@@ -199,38 +227,91 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedCache c, Page
     for (int i = 0; i < 8; ++i) acc[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  for (int k0 = begin + wave * 32; k0 < end; k0 += 128) {
-    // the slot of key k0 + lane % 32; past the end, the last key's again
-    const int mine = slot_of(c, table, min(k0 + (lane & 31), end - 1));
+  // Past the end the last key's block stands in: what is read there is masked.
+  // RUNS: the blocks of the step's two tiles and where in them the tiles begin;
+  // otherwise the block of key k0 + lane % 32.
+  const int k_first = begin + wave * 32;
+  auto last_at = [&](int k) { return min(k, end - 1); };
+  auto block_at = [&](int k) { return table[(uint32_t)last_at(k) / (uint32_t)c.block]; };
+  const int mine = RUNS ? 0 : lane & 31;
+  int ahead[2] = {0, 0};
+  if (k_first < end) {
+    ahead[0] = block_at(k_first + mine);
+    if (RUNS) ahead[1] = block_at(k_first + 16);
+  }
+  int slot[2], slot_next[2];  // of the tiles' first keys, or [0] of key k0 + mine
+  auto slots_at = [&](int k0, int (&to)[2]) {  // takes the ids asked for, asks for the next ones
+    auto slot_in = [&](int id, int k) {
+      const int at = (int)((uint32_t)last_at(k) % (uint32_t)c.block);
+      return id < 0 || id >= c.n_blocks ? -1 : id * c.block + (RUNS ? at & ~15 : at);
+    };
+    to[0] = slot_in(ahead[0], k0 + mine);
+    to[1] = RUNS ? slot_in(ahead[1], k0 + 16) : 0;
+    if (RUNS) {
+      to[0] = __builtin_amdgcn_readfirstlane(to[0]);
+      to[1] = __builtin_amdgcn_readfirstlane(to[1]);
+    }
+    ahead[0] = block_at(k0 + 128 + mine);
+    if (RUNS) ahead[1] = block_at(k0 + 144);
+  };
+  // 16 copies of four whole rows each, in 16-byte pieces; K's pieces are laid
+  // out so that the 16 keys of a fragment read distinct banks
+  const uint32_t ld = (uint32_t)c.ld * 2u;  // bytes
+  uint32_t k_off[4], v_off[4];              // in a tile
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    k_off[i] = (RUNS ? (i * 4 + lg) * ld : 0) + (ln ^ (i * 4 + lg)) * 16;
+    v_off[i] = (RUNS ? (i * 4 + lg) * ld : 0) + ln * 16;
+  }
+  auto copy_rows = [&](const int (&from)[2]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int first = RUNS ? from[i >> 2] : __shfl(from[0], i * 4 + lg);
+      const uint64_t at = (uint64_t)(uint32_t)max(first, 0) * ld;
+      dma16((const char*)kp + at + k_off[i & 3], s_mine[wave].rows[0] + i * 1024);
+      dma16((const char*)vp + at + v_off[i & 3], s_mine[wave].rows[1] + i * 1024);
+    }
+  };
+  if (k_first < end) {
+    slots_at(k_first, slot_next);
+    copy_rows(slot_next);
+  }
+  for (int k0 = k_first; k0 < end; k0 += 128) {
+    slot[0] = slot_next[0];
+    slot[1] = slot_next[1];
+    wait_vmcnt<0>();
+    asm volatile("" ::: "memory");
     u32x4 kr[2][4], vr[8];
-    int ks[2], vs[8];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      ks[t] = __shfl(mine, t * 16 + ln);
-      const bf16* src = kp + (int64_t)max(ks[t], 0) * c.ld + lg * 8;
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) kr[t][k] = *reinterpret_cast<const u32x4*>(src + k * 32);
+      for (int k = 0; k < 4; ++k)
+        kr[t][k] = *reinterpret_cast<const u32x4*>(s_mine[wave].rows[0] + (t * 16 + ln) * 256 + ((k * 4 + lg) ^ ln) * 16);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      vr[e] = *reinterpret_cast<const u32x4*>(s_mine[wave].rows[1] + ((e & 4) * 4 + lg * 4 + (e & 3)) * 256 + ln * 16);
+    wait_lgkmcnt<0>();  // the rows are read before the next ones come
+    asm volatile("" ::: "memory");
+    if (k0 + 128 < end) {
+      slots_at(k0 + 128, slot_next);
+      copy_rows(slot_next);
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      vs[e] = __shfl(mine, (e & 4) * 4 + lg * 4 + (e & 3));
-      vr[e] = *reinterpret_cast<const u32x4*>(vp + (int64_t)max(vs[e], 0) * c.ld + ln * 8);
-    }
-    if (__ballot(mine < 0)) {  // keys without a slot are zeros
+    if (RUNS ? (slot[0] | slot[1]) < 0 : __ballot(slot[0] < 0) != 0) {  // keys without a slot are zeros
 #pragma unroll
       for (int t = 0; t < 2; ++t)
+        if ((RUNS ? slot[t] : __shfl(slot[0], t * 16 + ln)) < 0)
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (ks[t] < 0) kr[t][k] = u32x4{0, 0, 0, 0};
+          for (int k = 0; k < 4; ++k) kr[t][k] = u32x4{0, 0, 0, 0};
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (vs[e] < 0) vr[e] = u32x4{0, 0, 0, 0};
+        if ((RUNS ? slot[e >> 2] : __shfl(slot[0], (e & 4) * 4 + lg * 4 + (e & 3))) < 0) vr[e] = u32x4{0, 0, 0, 0};
     }
     // An infinity or NaN of V at a key that some query does not attend to must
     // not reach it through a weight of 0: such elements are left out of the
     // product and added for the queries that do attend.
+    const bool partly = k0 + 32 > shortest;
     bool odd = false;
-    if (k0 + 32 > shortest) {
+    if (partly) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
 #pragma unroll
@@ -241,10 +322,10 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedCache c, Page
         for (int e = 0; e < 8; ++e)
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
-            uint32_t x = vr[e][w];
-            if ((x & 0x7F80u) == 0x7F80u) x &= 0xFFFF0000u;
-            if ((x & 0x7F800000u) == 0x7F800000u) x &= 0xFFFFu;
-            vr[e][w] = x;
+            uint32_t y = vr[e][w];
+            if ((y & 0x7F80u) == 0x7F80u) y &= 0xFFFF0000u;
+            if ((y & 0x7F800000u) == 0x7F800000u) y &= 0xFFFFu;
+            vr[e][w] = y;
           }
       }
     }
@@ -261,56 +342,82 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedCache c, Page
       va[2 * w] = __builtin_bit_cast(bf16x8, even);
       va[2 * w + 1] = __builtin_bit_cast(bf16x8, odds);
     }
+    // the tiles of queries side by side, so that one's waits are the other's work
+    f32x4 s[QT][2];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) s[t][0] = s[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) s[t][h] = mfma16(__builtin_bit_cast(bf16x8, kr[h][k]), qf[t][k], s[t][h]);
+    if (partly)
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[t][h][j] = k0 + h * 16 + lg * 4 + j < klen[t] ? s[t][h][j] : -INFINITY;
+    float top[QT];
+    bool rises = false;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) s[h] = mfma16(__builtin_bit_cast(bf16x8, kr[h][k]), qf[t][k], s[h]);
-      float top = m[t];
+      top[t] = -INFINITY;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          s[h][j] = k0 + h * 16 + lg * 4 + j < klen[t] ? s[h][j] * scale : -INFINITY;
-          top = fmaxf(top, s[h][j]);
-        }
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      if (__ballot(top > m[t])) {
-        const float f = m[t] == top ? 1.f : __builtin_amdgcn_exp2f(m[t] - top);
+        for (int j = 0; j < 4; ++j) top[t] = fmaxf(top[t], s[t][h][j]);
+    }
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      top[t] = most_of_four(top[t]);
+      rises |= top[t] > m[t] + kSlack / scale;
+    }
+    if (__ballot(rises))
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        const bool up = top[t] > m[t] + kSlack / scale;
+        const float f = up ? __builtin_amdgcn_exp2f((m[t] - top[t]) * scale) : 1.f;
         l[t] *= f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[t][i] *= f;
-        m[t] = top;
+        m[t] = up ? top[t] : m[t];
       }
-      const float from = top == -INFINITY ? 0.f : top;
-      bf16x8 pf;
+    bf16x8 pf[QT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      const float from = m[t] == -INFINITY ? 0.f : m[t] * scale;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float w = __builtin_amdgcn_exp2f(s[h][j] - from);
-          s[h][j] = w;
+          const float w = __builtin_amdgcn_exp2f(fmaf(s[t][h][j], scale, -from));
+          s[t][h][j] = w;
           l[t] += w;
-          pf[h * 4 + j] = (bf16)w;
+          pf[t][h * 4 + j] = (bf16)w;
         }
+    }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[t][i] = mfma16(va[i], pf, acc[t][i]);
-      if (odd) {
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int t = 0; t < QT; ++t) acc[t][i] = mfma16(va[i], pf[t], acc[t][i]);
+    if (odd) {
 #pragma unroll 1
-        for (int key = 0; key < 32; ++key) {
+      for (int key = 0; key < 32; ++key) {
+        const int run = slot[key >> 4 & (RUNS ? 1 : 0)];
+        const int64_t at = RUNS ? (run < 0 ? -1 : run + (key & 15)) : __shfl(slot[0], key);
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
           float w = 0.f;
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-              if (key >> 4 == h && (key & 3) == j) w = s[h][j];
+              if (key >> 4 == h && (key & 3) == j) w = s[t][h][j];
           w = (float)(bf16)__shfl(w, (key & 12) * 4 + ln);
-          const int64_t slot = __shfl(mine, key);
-          const bool seen = k0 + key < klen[t] && slot >= 0;
-          const bf16* src = vp + (seen ? slot * c.ld : 0) + lg * 32;
+          const bool seen = k0 + key < klen[t] && at >= 0;
+          const bf16* src = vp + (seen ? at * c.ld : 0) + lg * 32;
 #pragma unroll
           for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -323,63 +430,80 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedCache c, Page
     }
   }
 
-  // the four waves' results, one tile of queries after the other
+  // the four waves' results
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     float sum = l[t] + __shfl_xor(l[t], 16);
     sum += __shfl_xor(sum, 32);
     if (lg == 0) {
-      s_m[wave][ln] = m[t];
-      s_l[wave][ln] = sum;
+      s_m[wave][t * 16 + ln] = m[t] * scale;
+      s_l[wave][t * 16 + ln] = sum;
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
       for (int i = 0; i < 8; i += 4)
-        *reinterpret_cast<f32x4*>(&s_out[wave][ln][(lg * 4 + e) * 8 + i]) =
+        *reinterpret_cast<f32x4*>(&s_mine[wave].out[t * 16 + ln][(lg * 4 + e) * 8 + i]) =
             f32x4{acc[t][i][e], acc[t][i + 1][e], acc[t][i + 2][e], acc[t][i + 3][e]};
-    __syncthreads();
-    const int n = threadIdx.x >> 4, d = (threadIdx.x & 15) * 8, q = q0 + t * 16 + n;
-    if (q < nq) {
-      float top = s_m[0][n];
+  }
+  __syncthreads();
 #pragma unroll
-      for (int w = 1; w < 4; ++w) top = fmaxf(top, s_m[w][n]);
-      const float from = top == -INFINITY ? 0.f : top;
-      float total = 0.f, o[8] = {};
+  for (int t = 0; t < QT; ++t) {
+    const int n = t * 16 + (threadIdx.x >> 4), d = (threadIdx.x & 15) * 8, q = q0 + n;
+    if (q >= nq) continue;
+    float top = s_m[0][n];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float f = s_m[w][n] == top ? 1.f : __builtin_amdgcn_exp2f(s_m[w][n] - from);
-        total += s_l[w][n] * f;
-        if (s_l[w][n] != 0.f)
+    for (int w = 1; w < 4; ++w) top = fmaxf(top, s_m[w][n]);
+    const float from = top == -INFINITY ? 0.f : top;
+    float total = 0.f, o[8] = {};
 #pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] += s_out[w][n][d + e] * f;
-      }
-      const int i = q / rep, h = gr.g * rep + q - i * rep;
-      const int64_t row = (int64_t)gr.b * r.per_request + i;
-      if (p.splits == 1) {
-        const float inv = total == 0.f ? 0.f : 1.f / total;
-        bf16x8 v;
+    for (int w = 0; w < 4; ++w) {
+      const float f = s_m[w][n] == top ? 1.f : __builtin_amdgcn_exp2f(s_m[w][n] - from);
+      total += s_l[w][n] * f;
+      if (s_l[w][n] != 0.f)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = (bf16)(o[e] * inv);
-        *reinterpret_cast<bf16x8*>((bf16*)r.out + row * r.out_ld + h * 128 + d) = v;
-        if (r.lse && d == 0) r.lse[row * r.heads + h] = (from + __builtin_amdgcn_logf(total)) * kLn2;
-      } else {
-        const int64_t at = ((int64_t)gr.split * c.batch * r.per_request + row) * r.heads + h;
-        *reinterpret_cast<f32x4*>(p.part + at * 128 + d) = f32x4{o[0], o[1], o[2], o[3]};
-        *reinterpret_cast<f32x4*>(p.part + at * 128 + d + 4) = f32x4{o[4], o[5], o[6], o[7]};
-        if (d == 0) p.stats[at] = make_float2(top, total);
-      }
+        for (int e = 0; e < 8; ++e) o[e] += s_mine[w].out[n][d + e] * f;
     }
-    __syncthreads();
+    const int i = q / rep, h = gr.g * rep + q - i * rep;
+    const int64_t row = (int64_t)gr.b * r.per_request + i;
+    if (p.splits == 1) {
+      const float inv = total == 0.f ? 0.f : 1.f / total;
+      bf16x8 v;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = (bf16)(o[e] * inv);
+      *reinterpret_cast<bf16x8*>((bf16*)r.out + row * r.out_ld + h * 128 + d) = v;
+      if (r.lse && d == 0) r.lse[row * r.heads + h] = (from + __builtin_amdgcn_logf(total)) * kLn2;
+    } else {
+      const int64_t at = ((int64_t)gr.split * c.batch * r.per_request + row) * r.heads + h;
+      *reinterpret_cast<f32x4*>(p.part + at * 128 + d) = f32x4{o[0], o[1], o[2], o[3]};
+      *reinterpret_cast<f32x4*>(p.part + at * 128 + d + 4) = f32x4{o[4], o[5], o[6], o[7]};
+      if (d == 0) p.stats[at] = make_float2(top, total);
+    }
   }
 }
 
 // fp32: 16 lanes share a key (elements lane % 16 + 16 i), a wave four keys at a
-// time; every 16 lanes keep a running softmax of their own for the tile's four
-// queries.
+// time, four such on their way; every 16 lanes keep a running softmax of their
+// own for the tile's four queries.
 constexpr int kQueriesF32 = 4;
+
+// The sum over the 16 lanes of a row, in each of them (moves in registers: by
+// half the row, a quarter, ...).
+template <int ROR>
+__device__ __forceinline__ float turned_row(float v) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x120 + ROR, 0xF, 0xF, false));
+}
+__device__ __forceinline__ float row_sum(float v) {
+  v += turned_row<8>(v);
+  v += turned_row<4>(v);
+  v += turned_row<2>(v);
+  v += turned_row<1>(v);
+  return v;
+}
+
+template <int N>  // elements of a head that a lane has, head_dim <= 16 N
 __global__ __launch_bounds__(256) void paged_attention_f32_kernel(PagedCache c, PagedQueries r, PagedPlan p) {
-  constexpr int Q = kQueriesF32;
+  constexpr int Q = kQueriesF32, U = 4;
   __shared__ float s_out[16][128];
   __shared__ float s_m[16], s_l[16];
   Group gr;
@@ -387,7 +511,7 @@ __global__ __launch_bounds__(256) void paged_attention_f32_kernel(PagedCache c, 
   const int ln = threadIdx.x & 15, str = threadIdx.x >> 4;  // 16 streams of keys
   const int rep = r.heads / c.kv_heads, nq = r.per_request * rep, q0 = gr.tile * Q, d = c.head_dim;
   int klen[Q], longest = 0;
-  float q[Q][8], m[Q], l[Q], acc[Q][8];
+  float q[Q][N], m[Q], l[Q], acc[Q][N];
   const float scale = kLog2e / sqrtf((float)d);
 #pragma unroll
   for (int t = 0; t < Q; ++t) {
@@ -400,7 +524,7 @@ __global__ __launch_bounds__(256) void paged_attention_f32_kernel(PagedCache c, 
     m[t] = -INFINITY;
     l[t] = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < N; ++e) {
       q[t][e] = ln + 16 * e < d ? src[ln + 16 * e] * scale : 0.f;
       acc[t][e] = 0.f;
     }
@@ -408,32 +532,38 @@ __global__ __launch_bounds__(256) void paged_attention_f32_kernel(PagedCache c, 
   int begin, end;
   share_of(longest, p.splits, gr.split, begin, end);
   const int32_t* table = c.tables + (int64_t)gr.b * c.table_ld;
-  for (int k = begin + str; k < end; k += 16) {
-    const int slot = slot_of(c, table, k);
-    const int64_t off = (int64_t)max(slot, 0) * c.ld + gr.g * d;
-    float kv[8], vv[8];
+  for (int k0 = begin + str; k0 < end; k0 += 16 * U) {
+    int slot[U];
+    float kv[U][N], vv[U][N];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const bool in = slot >= 0 && ln + 16 * e < d;
-      kv[e] = in ? ((const float*)c.k)[off + ln + 16 * e] : 0.f;
-      vv[e] = in ? ((const float*)c.v)[off + ln + 16 * e] : 0.f;
+    for (int u = 0; u < U; ++u) slot[u] = k0 + 16 * u < end ? slot_of(c, table, k0 + 16 * u) : -1;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t off = (int64_t)max(slot[u], 0) * c.ld + gr.g * d;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const bool in = slot[u] >= 0 && ln + 16 * e < d;
+        kv[u][e] = in ? ((const float*)c.k)[off + ln + 16 * e] : 0.f;
+        vv[u][e] = in ? ((const float*)c.v)[off + ln + 16 * e] : 0.f;
+      }
     }
 #pragma unroll
-    for (int t = 0; t < Q; ++t) {
-      float s = 0.f;
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s += q[t][e] * kv[e];
+      for (int t = 0; t < Q; ++t) {
+        float s = 0.f;
 #pragma unroll
-      for (int o = 8; o > 0; o >>= 1) s += __shfl_xor(s, o);
-      if (k >= klen[t] || s == -INFINITY) continue;  // uniform over the 16 lanes
-      const float top = fmaxf(m[t], s);
-      const float f = m[t] == top ? 1.f : __builtin_amdgcn_exp2f(m[t] - top);
-      const float w = __builtin_amdgcn_exp2f(s - top);
-      l[t] = l[t] * f + w;
-      m[t] = top;
+        for (int e = 0; e < N; ++e) s += q[t][e] * kv[u][e];
+        s = row_sum(s);
+        if (k0 + 16 * u >= klen[t] || s == -INFINITY) continue;  // uniform over the 16 lanes
+        const float top = fmaxf(m[t], s);
+        const float f = m[t] == top ? 1.f : __builtin_amdgcn_exp2f(m[t] - top);
+        const float w = __builtin_amdgcn_exp2f(s - top);
+        l[t] = l[t] * f + w;
+        m[t] = top;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[t][e] = acc[t][e] * f + w * vv[e];
-    }
+        for (int e = 0; e < N; ++e) acc[t][e] = acc[t][e] * f + w * vv[u][e];
+      }
   }
 #pragma unroll
   for (int t = 0; t < Q; ++t) {
@@ -442,7 +572,7 @@ __global__ __launch_bounds__(256) void paged_attention_f32_kernel(PagedCache c, 
       s_l[str] = l[t];
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s_out[str][ln + 16 * e] = acc[t][e];
+    for (int e = 0; e < N; ++e) s_out[str][ln + 16 * e] = acc[t][e];
     __syncthreads();
     if (q0 + t < nq && (int)threadIdx.x < d) {
       float top = s_m[0];
@@ -469,41 +599,79 @@ __global__ __launch_bounds__(256) void paged_attention_f32_kernel(PagedCache c, 
   }
 }
 
-// Joins the splits of a (row, head) in their order; a split without keys has a
-// sum of 0 and is not read.  One wave, lane l elements 2 l and 2 l + 1.
-template <typename T>
+// Joins the splits of a (row, head), a split without keys (sum 0) is not read.
+// WAVES waves take every WAVES-th split, eight at a time, lane l elements 2 l and
+// 2 l + 1, and are added in their order.
+template <typename T, int WAVES>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedCache c, PagedQueries r, PagedPlan p) {
+  __shared__ float2 s_part[WAVES > 1 ? WAVES : 1][64];
   const int64_t pairs = (int64_t)c.batch * r.per_request * r.heads;
-  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), d = c.head_dim;
+  const int64_t at = WAVES > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
   if (at >= pairs) return;
-  const int lane = threadIdx.x & 63, d = c.head_dim;
+  constexpr int NS = (kMaxSplits + 63) / 64;
+  float2 st[NS];
   float top = -INFINITY;
-  for (int s = lane; s < p.splits; s += 64) top = fmaxf(top, p.stats[s * pairs + at].x);
+#pragma unroll
+  for (int i = 0; i < NS; ++i) {
+    st[i] = make_float2(-INFINITY, 0.f);
+    if (i * 64 < p.splits && i * 64 + lane < p.splits) st[i] = p.stats[(i * 64 + lane) * pairs + at];
+    top = fmaxf(top, st[i].x);
+  }
   top = wave_max(top);
   const float from = top == -INFINITY ? 0.f : top;
-  float total = 0.f, o[2] = {0.f, 0.f};
-  for (int s = 0; s < p.splits; ++s) {
-    const float2 st = p.stats[s * pairs + at];
-    if (st.y == 0.f) continue;
-    const float f = st.x == top ? 1.f : __builtin_amdgcn_exp2f(st.x - from);
-    total += st.y * f;
-    if (2 * lane < d) {
-      const float2 v = *reinterpret_cast<const float2*>(p.part + (s * pairs + at) * d + 2 * lane);
-      o[0] += v.x * f;
-      o[1] += v.y * f;
+  float total = 0.f, f[NS];
+#pragma unroll
+  for (int i = 0; i < NS; ++i) {
+    f[i] = st[i].x == top ? 1.f : __builtin_amdgcn_exp2f(st[i].x - from);
+    total += st[i].y * f[i];
+    if (st[i].y == 0.f) f[i] = 0.f;
+  }
+  total = wave_sum(total);
+  float2 o = make_float2(0.f, 0.f);
+  const float* part = p.part + at * d + 2 * lane;
+#pragma unroll
+  for (int i = 0; i < NS; ++i) {
+    if (i * 64 >= p.splits) break;
+    const int n = min(64, p.splits - i * 64);
+    for (int j0 = WAVES > 1 ? wave : 0; j0 < n; j0 += 8 * WAVES) {
+      float2 v[8];
+      float w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int s = j0 + j * WAVES;
+        w[j] = s < n ? __shfl(f[i], s) : 0.f;
+        v[j] = make_float2(0.f, 0.f);
+        if (w[j] != 0.f && 2 * lane < d) v[j] = *reinterpret_cast<const float2*>(part + (int64_t)(i * 64 + s) * pairs * d);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        o.x += v[j].x * w[j];
+        o.y += v[j].y * w[j];
+      }
+    }
+  }
+  if constexpr (WAVES > 1) {
+    s_part[wave][lane] = o;
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) {
+      o.x += s_part[w][lane].x;
+      o.y += s_part[w][lane].y;
     }
   }
   const int64_t row = at / r.heads, h = at - row * r.heads;
   if (2 * lane < d) {
     const float inv = total == 0.f ? 0.f : 1.f / total;
     T* dst = (T*)r.out + row * r.out_ld + h * d + 2 * lane;
-    dst[0] = from_f32<T>(o[0] * inv);
-    dst[1] = from_f32<T>(o[1] * inv);
+    dst[0] = from_f32<T>(o.x * inv);
+    dst[1] = from_f32<T>(o.y * inv);
   }
   if (r.lse && lane == 0) r.lse[at] = (from + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
-int tile_queries(int queries, bool f32) { return f32 ? kQueriesF32 : queries <= 16 ? 16 : queries <= 32 ? 32 : 64; }
+int tile_queries(int queries, bool f32) { return f32 ? kQueriesF32 : queries <= 16 ? 16 : 32; }
 
 }  // namespace
 
@@ -532,10 +700,32 @@ PagedPlan plan_paged_attention(acache_dtype dt, const PagedCache& c, int per_req
   p.tiles = (queries + p.tile - 1) / p.tile;
   const int64_t groups = (int64_t)c.batch * c.kv_heads * p.tiles;
   const int64_t pairs = (int64_t)c.batch * per_request * heads;
-  // two workgroups for every CU, none with less than 128 keys
-  int64_t splits = std::min<int64_t>((512 + groups - 1) / groups, (max_len + 127) / 128);
   const size_t each = (size_t)pairs * (c.head_dim + 2) * sizeof(float);
-  splits = std::min<int64_t>(splits, (int64_t)(ws_bytes / std::max<size_t>(each, 1)));
+  const int64_t most = std::min<int64_t>({(max_len + 127) / 128, kMaxSplits, (int64_t)(ws_bytes / std::max<size_t>(each, 1))});
+  // The split with the least estimated time, in us.  Workgroups run two a CU, in
+  // rounds; one takes a step for every 128 keys.  A step is the longest of a
+  // chain of dependent waits that grows with the load, the rate of the memory for
+  // all that run (6 TB/s; tiles of the same keys read them once), and the work of
+  // those that share a CU.  The join is a launch, and the partials' way.  One row
+  // of 8 requests over 30011 keys, 4 KV heads: 323 us unsplit, 99 in 5 parts, 85
+  // in 8, 84 in 16, 92 in 32; 4 x 32 rows of 28 heads over 5120 keys: 48, 2 parts
+  // 34, 4 parts 30, 8 parts 34.
+  const bool wide = p.tile == 32, f32 = dt == ACACHE_F32;
+  const double chain = f32 ? 2.0 : wide ? 1.1 : 1.3, work = f32 ? 1.5 : wide ? 1.05 : 0.6;
+  int64_t splits = 1;
+  double best = 1e30;
+  for (int64_t s = 1; s <= std::max<int64_t>(most, 1); ++s) {
+    const int64_t n = groups * s, running = std::min<int64_t>(n, 512);
+    const double read = running * 256.0 * c.head_dim * (f32 ? 4 : 2) / 6e6 / p.tiles;
+    const double step = std::max({chain + 0.35 * read, read, work * (double)((running + 255) / 256)});
+    const double steps = (double)(((max_len + s - 1) / s + 127) / 128);
+    const double us = 4.0 + (steps * step + 1.6) * (n > 512 ? n / 512.0 + 0.3 : 1.0) +
+                      (s > 1 ? 4.0 + 0.05 * s + (double)s * pairs * c.head_dim / 1e6 : 0.0);
+    if (us < best) {
+      best = us;
+      splits = s;
+    }
+  }
   p.splits = (int)std::max<int64_t>(splits, 1);
   p.ws_bytes = p.splits > 1 ? p.splits * each : 0;
   return p;
@@ -549,14 +739,23 @@ hipError_t launch_paged_attention(acache_dtype dt, const PagedCache& c, const Pa
   p.stats = (float2*)(p.part + pairs * p.splits * c.head_dim);
   const int64_t keys = (int64_t)c.batch * c.kv_heads * p.splits;
   const dim3 grid((unsigned)((keys + 7) / 8 * 8 * p.tiles));
-  if (dt == ACACHE_F32) hipLaunchKernelGGL(paged_attention_f32_kernel, grid, dim3(256), 0, s, c, r, p);
-  else if (p.tile == 16) hipLaunchKernelGGL(paged_attention_kernel<1>, grid, dim3(256), 0, s, c, r, p);
-  else if (p.tile == 32) hipLaunchKernelGGL(paged_attention_kernel<2>, grid, dim3(256), 0, s, c, r, p);
-  else hipLaunchKernelGGL(paged_attention_kernel<4>, grid, dim3(256), 0, s, c, r, p);
+  const bool runs = c.block % 16 == 0 && c.ld < 1 << 26;  // 16 rows within 2^31 bytes
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, c, r, p); };
+  if (dt == ACACHE_F32) {
+    if (c.head_dim <= 32) go(paged_attention_f32_kernel<2>);
+    else if (c.head_dim <= 64) go(paged_attention_f32_kernel<4>);
+    else go(paged_attention_f32_kernel<8>);
+  } else {
+    if (p.tile == 16) runs ? go(paged_attention_kernel<1, true>) : go(paged_attention_kernel<1, false>);
+    else runs ? go(paged_attention_kernel<2, true>) : go(paged_attention_kernel<2, false>);
+  }
   if (p.splits > 1) {
-    const dim3 merge((unsigned)((pairs + 3) / 4));
-    if (dt == ACACHE_F32) hipLaunchKernelGGL(paged_merge_kernel<float>, merge, dim3(256), 0, s, c, r, p);
-    else hipLaunchKernelGGL(paged_merge_kernel<bf16>, merge, dim3(256), 0, s, c, r, p);
+    // one wave a pair with few splits, else four
+    const dim3 few((unsigned)((pairs + 3) / 4)), many((unsigned)pairs);
+    if (dt == ACACHE_F32 && p.splits <= 8) hipLaunchKernelGGL((paged_merge_kernel<float, 1>), few, dim3(256), 0, s, c, r, p);
+    else if (dt == ACACHE_F32) hipLaunchKernelGGL((paged_merge_kernel<float, 4>), many, dim3(256), 0, s, c, r, p);
+    else if (p.splits <= 8) hipLaunchKernelGGL((paged_merge_kernel<bf16, 1>), few, dim3(256), 0, s, c, r, p);
+    else hipLaunchKernelGGL((paged_merge_kernel<bf16, 4>), many, dim3(256), 0, s, c, r, p);
   }
   return hipGetLastError();
 }
