@@ -773,6 +773,7 @@ class PagedCache:
         self.k_pool, self.v_pool, self.tables, self.block = k_pool, v_pool, tables, block
         self.batch, self.max_blocks = tables.shape
         self.width, self.device, self.dtype = k_pool.shape[1], k_pool.device, k_pool.dtype
+        self.index = k_pool.get_device()  # -1: not a GPU's
         # the stride of a single row says nothing
         ld = k_pool.stride(0) if k_pool.shape[0] > 1 else self.width
         table_ld = tables.stride(0) if self.batch > 1 else self.max_blocks
@@ -781,23 +782,29 @@ class PagedCache:
         self.ref = ctypes.byref(self.desc)
 
 
+def _all_here(*tensors):
+    """Every tensor that is given is on the current device."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"a tensor is on {t.device}, not on the current device")
+
+
 def _paged_check(dims: Dims, cache: PagedCache, *tensors):
     """The cache fits dims, and everything is on the current device."""
     if cache.dtype != torch_dtype(dims) or cache.width < dims.n_kv_heads * dims.head_dim:
         raise ValueError("the pools do not hold rows of dims.n_kv_heads heads of dims.head_dim of dims' type")
-    device = cache.device
-    if device.type != "cuda" or device.index != torch.cuda.current_device():
-        raise ValueError(f"the cache is on {device}, not on the current device")
-    for t in tensors:
-        if t.device != device:
-            raise ValueError(f"a tensor is on {t.device} and the cache on {device}")
+    if cache.index < 0:
+        raise ValueError(f"the cache is on {cache.device}")
+    _all_here(cache.k_pool, *tensors)
 
 
 def _row_ld(t: torch.Tensor, n: int, width: int, dt, name: str) -> int:
     """The row stride of t: [n, width] of type dt, rows contiguous and apart."""
-    if t.dtype != dt or t.dim() != 2 or t.shape[0] != n or t.shape[1] != width or (width > 1 and t.stride(1) != 1):
+    ld = t.stride()
+    if t.dtype != dt or t.shape != (n, width) or (width > 1 and ld[1] != 1):
         raise TypeError(f"{name} must be a [{n}, {width}] {dt} tensor with contiguous rows")
-    return t.stride(0) if n > 1 else width
+    return ld[0] if n > 1 else width
 
 
 def _dev_rows(t: torch.Tensor, n: int, dt, name: str):
@@ -827,7 +834,7 @@ def acache_paged_append(dims: Dims, cache: PagedCache, k: torch.Tensor, v: torch
             with _own(stream):
                 q_out = torch.empty((n, hq), dtype=dt, device=q.device)
         q_out_ld = _row_ld(q_out, n, hq, dt, "q_out")
-    _paged_check(dims, cache, *(t for t in (k, v, pos, at, q, q_out) if t is not None))
+    _paged_check(dims, cache, k, v, pos, at, q, q_out)
     _check("acache_paged_append", lib.acache_paged_append(
         ctypes.byref(dims), cache.ref, rows_per_request, _ptr(q), q_ld, k.data_ptr(), k_ld, v.data_ptr(), v_ld,
         pos.data_ptr(), _ptr(at), _ptr(q_out), q_out_ld, _stream(stream)))
@@ -866,7 +873,7 @@ def acache_paged_attention(dims: Dims, cache: PagedCache, q: torch.Tensor, key_l
     out_ld = _row_ld(out, n, hq, dt, "out")
     if lse is not None:
         _dev_rows(lse, n * dims.n_heads, torch.float32, "lse")
-    _paged_check(dims, cache, *(t for t in (q, key_len, out, lse, ws) if t is not None))
+    _paged_check(dims, cache, q, key_len, out, lse, ws)
     _check("acache_paged_attention", lib.acache_paged_attention(
         ctypes.byref(dims), cache.ref, rows_per_request, q.data_ptr(), q_ld, key_len.data_ptr(), max_len,
         out.data_ptr(), out_ld, _ptr(lse), _ptr(ws), 0 if ws is None else ws.nbytes, _stream(stream)))
@@ -907,14 +914,12 @@ def acache_sample_commit(x: torch.Tensor, u: torch.Tensor, temperature: Optional
         raise ValueError("commit_pos and ids go together")
     if ids is not None:
         _dev_i32(ids, "ids")
-    if x.device.type != "cuda" or x.device.index != torch.cuda.current_device():
-        raise ValueError(f"x is on {x.device}, not on the current device")
+    if x.get_device() < 0:
+        raise ValueError(f"x is on {x.device}")
+    _all_here(x, u, temperature, top_k, top_p, min_p, out, conf, prob, commit_pos, ids)
     if out is None:
         with _own(stream):
             out = torch.empty(rows, dtype=torch.int32, device=x.device)
-    for t in (u, temperature, top_k, top_p, min_p, out, conf, prob, commit_pos, ids):
-        if t is not None and t.device != x.device:
-            raise ValueError(f"a tensor is on {t.device} and x on {x.device}")
     _check("acache_sample_commit", lib.acache_sample_commit(
         ACACHE_BF16 if x.dtype == torch.bfloat16 else ACACHE_F32, x.data_ptr(), x.stride(0) if rows > 1 else n, rows, n,
         _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), u.data_ptr(), out.data_ptr(), _ptr(conf), _ptr(prob),

@@ -157,13 +157,11 @@ __device__ __forceinline__ float most_of_four(float v) {
 // waves keep 128 KB in flight, several times what the memory's latency asks for
 // at a CU's share of its rate.  The block ids of the next step's keys are on
 // their way meanwhile.
-// The running maximum is raised only where the logits pass it by kSlack powers
-// of two (weights then reach 2^kSlack, which their types hold as well): with
-// random keys it rises for some query at almost every step, and each rise
-// scales the whole output.
 // A weight is rounded to bf16 for its product with V (2^-8 relative at most); its sum
-// is of the unrounded ones.
-constexpr float kSlack = 8.f;
+// is of the unrounded ones.  The maximum is kept exactly, so that the largest
+// weight is 1, which rounding leaves as it is: raising it only in steps of 2^8
+// saves 6% with 224 queries of a KV head, and takes the error against 64 bits
+// from 0.0019 to 0.0026.
 // RUNS: blocks are of whole runs of 16 slots, so that the 16 keys of a tile lie
 // one behind the other: their rows are a scalar base and per-lane offsets that
 // do not change.  Otherwise every lane finds the slot of one key and the others
@@ -372,12 +370,12 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedCache c, P
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
       top[t] = most_of_four(top[t]);
-      rises |= top[t] > m[t] + kSlack / scale;
+      rises |= top[t] > m[t];
     }
     if (__ballot(rises))
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
-        const bool up = top[t] > m[t] + kSlack / scale;
+        const bool up = top[t] > m[t];
         const float f = up ? __builtin_amdgcn_exp2f((m[t] - top[t]) * scale) : 1.f;
         l[t] *= f;
 #pragma unroll
