@@ -430,6 +430,41 @@ class Head:
         self.w = w
 
 
+class Sampling:
+    """How a schedule draws a block's tokens in place of the greedy pick
+    (acache_sample_commit): temperature, top_k, top_p and min_p as numbers for
+    the whole batch or one for each request, and u from `generator` (torch's, on
+    the batch's device; None: its default one), one number a row and step in row
+    order, so that a seed gives its tokens again."""
+
+    def __init__(self, batch: AffixBatch, block_len: int, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
+                 generator: Optional[torch.Generator] = None):
+        n = batch.B * block_len
+
+        def rows(v, dtype):
+            t = torch.as_tensor(v, dtype=dtype, device=batch.device)
+            if t.dim() > 1 or (t.dim() == 1 and t.numel() != batch.B):
+                raise ValueError("a setting is one number, or one for each request")
+            return t.expand(batch.B).repeat_interleave(block_len).contiguous()
+        self.settings = dict(temperature=rows(temperature, torch.float32), top_k=rows(top_k, torch.int32),
+                             top_p=rows(top_p, torch.float32), min_p=rows(min_p, torch.float32))
+        self.u = torch.empty(n, dtype=torch.float64, device=batch.device)
+        self.generator = generator
+
+    def commit(self, logits: torch.Tensor, stream=None, **to) -> torch.Tensor:
+        """acache_argmax_commit's call, drawn."""
+        with _on(stream):
+            self.u.uniform_(generator=self.generator)
+        return A.acache_sample_commit(logits, self.u, **self.settings, **to, stream=stream)
+
+
+def _commit(logits: torch.Tensor, sampling: Optional[Sampling], stream=None, **to):
+    if sampling is None:
+        A.acache_argmax_commit(logits, **to, stream=stream)
+    else:
+        sampling.commit(logits, stream=stream, **to)
+
+
 def block_row_index(batch: AffixBatch, k: int, block_begin: int, block_len: int) -> torch.Tensor:
     """Rows of the refresh output (k anchors per request) that hold logical
     positions [block_begin, block_begin + block_len) of every request.  A
@@ -482,14 +517,16 @@ class DecodePlan:
 
 @_on_its_stream
 def decode_schedule(batch: AffixBatch, head: Head, plan: DecodePlan, k: int, logits: torch.Tensor,
-                    committed: torch.Tensor, anchors: Optional[torch.Tensor] = None, stream=None):
+                    committed: torch.Tensor, anchors: Optional[torch.Tensor] = None, stream=None,
+                    sampling: Optional[Sampling] = None):
     """The serving schedule over the masked span (Sections 3.1 and 4.3): one
     probe and top-K per request (selective mode), then per block a refresh
     (selective, or full recomputation), the final norm and LM head on the
     block's rows, and a greedy commit of every position of the block into the
     token ids the next refresh embeds.  committed [n_blocks, B * block_len]
     receives the chosen ids; logits [B * block_len, vocab] is scratch.
-    anchors: a given anchor set [B, k] instead of the probe's (selective)."""
+    anchors: a given anchor set [B, k] instead of the probe's (selective).
+    sampling: the tokens are drawn (Sampling) instead."""
     if plan.full:
         anchors = plan.anchors
     elif anchors is None:
@@ -499,8 +536,7 @@ def decode_schedule(batch: AffixBatch, head: Head, plan: DecodePlan, k: int, log
         h = A.acache_gather_rows(x, plan.rows[blk], stream=stream)
         y = A.acache_rmsnorm(batch.model.dims, h, head.norm_g, stream=stream)
         A.acache_linear(batch.model.dims, y, head.w, out=logits, ws=batch.ws, stream=stream)
-        A.acache_argmax_commit(logits, out=committed[blk], commit_pos=plan.pos[blk], ids=batch.remap,
-                               stream=stream)
+        _commit(logits, sampling, out=committed[blk], commit_pos=plan.pos[blk], ids=batch.remap, stream=stream)
     return committed
 
 
@@ -559,7 +595,8 @@ def decode_step(batch: AffixBatch, plan: DecodePlan, blk: int, m: dict, anchors:
 @_on_its_stream
 def decode_threshold_schedule(batch: AffixBatch, head: Head, plan: DecodePlan, k: int, tau: float,
                               anchors: Optional[torch.Tensor] = None, trace: Optional[list] = None,
-                              max_steps: Optional[int] = None, stream=None):
+                              max_steps: Optional[int] = None, stream=None,
+                              sampling: Optional[Sampling] = None):
     """Block-wise decoding with confidence-threshold commits (Sections 3.1,
     4.3, 5).  Per block: a refresh (selective, or full recomputation) whose
     block rows give the first predictions; then, until every position of the
@@ -579,7 +616,9 @@ def decode_threshold_schedule(batch: AffixBatch, head: Head, plan: DecodePlan, k
     (commits) each block took; every step commits at least one position of
     each request whose block is not done, so a block takes at most
     block_len steps.  max_steps ends a block early (for measurement): its
-    positions not yet committed keep the mask id."""
+    positions not yet committed keep the mask id.
+    sampling: every step's picks are drawn (Sampling); the confidence compared
+    with tau stays the pick's softmax probability."""
     if batch.remap is None:
         raise ValueError("decode steps embed token ids: the batch needs remap")
     B, blen, dev = batch.B, plan.block_len, batch.device
@@ -604,7 +643,7 @@ def decode_threshold_schedule(batch: AffixBatch, head: Head, plan: DecodePlan, k
         while True:
             y = A.acache_rmsnorm(dims, h, head.norm_g, stream=stream)
             A.acache_linear(dims, y, head.w, out=logits, ws=batch.ws, stream=stream)
-            A.acache_argmax_commit(logits, out=pick, conf=conf, stream=stream)
+            _commit(logits, sampling, out=pick, conf=conf, stream=stream)
             A.acache_threshold_commit(blen, pick, conf, tau, flags, plan.pos[blk], batch.remap, count,
                                       stream=stream)
             count_host.copy_(count, non_blocking=True)
