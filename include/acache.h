@@ -596,7 +596,7 @@ typedef struct {
   const int32_t* tables; /* [batch, table_ld] block ids; entries that hold no attended position are not read */
   int64_t table_ld;      /* >= max_blocks */
   int32_t batch;
-  int32_t max_blocks;    /* entries of a request's table; max_blocks * block < 2^31 */
+  int32_t max_blocks;    /* entries of a request's table; max_blocks * block < 2^30 */
   int32_t block;         /* slots of a block, >= 1 */
 } acache_paged_cache;
 
@@ -637,7 +637,7 @@ acache_status acache_paged_append(const acache_dims* dims, const acache_paged_ca
  * tables' capacity); it sets how the keys are split over workgroups and nothing
  * else.  ws is optional: with acache_paged_workspace_size() bytes calls with
  * few rows split the keys (fp32 partials, joined in a fixed order); with less,
- * in fewer parts or none.  rows == 0: no-op. */
+ * in fewer parts or none.  rows < 2^30 and rows * H < 2^31.  rows == 0: no-op. */
 acache_status acache_paged_attention(const acache_dims* dims, const acache_paged_cache* cache, int32_t rows_per_request,
                                      const void* q, int64_t q_ld, const int32_t* key_len, int64_t max_len, void* out,
                                      int64_t out_ld, float* lse, void* ws, size_t ws_bytes, hipStream_t stream);

@@ -1163,7 +1163,7 @@ acache_status check_paged(const acache_dims* d, const acache_paged_cache* c, int
   CHECK(c->table_ld >= c->max_blocks && c->ld >= (int64_t)d->n_kv_heads * d->head_dim, ACACHE_ERR_SHAPE);
   constexpr int64_t k31 = (int64_t)1 << 31;
   CHECK(c->ld < k31 / 2, ACACHE_ERR_UNSUPPORTED);
-  CHECK(c->n_blocks < k31 && c->n_blocks * c->block < k31 && (int64_t)c->max_blocks * c->block < k31,
+  CHECK(c->n_blocks < k31 && c->n_blocks * c->block < k31 && (int64_t)c->max_blocks * c->block < k31 / 2,
         ACACHE_ERR_UNSUPPORTED);
   CHECK((int64_t)c->batch * rows_per_request < k31 / 2, ACACHE_ERR_UNSUPPORTED);
   out = PagedCache{c->k, c->v, c->ld, (int)c->n_blocks, c->block, d->n_kv_heads, d->head_dim, c->tables, c->table_ld,
@@ -1224,8 +1224,8 @@ acache_status acache_paged_attention(const acache_dims* dims, const acache_paged
           ACACHE_ERR_ALIGN);
   CHECK(!ws || aligned16(ws), ACACHE_ERR_ALIGN);
   const PagedPlan plan = plan_paged(dims, c, rows_per_request, max_len, ws ? ws_bytes : 0);
-  // one dimension of workgroups, of four (row, head) pairs each in the join
-  CHECK(((int64_t)c.batch * c.kv_heads * plan.splits + 8) * plan.tiles < (int64_t)1 << 31 && n * dims->n_heads < (int64_t)1 << 32,
+  // one dimension of workgroups, in the join one for a (row, head) pair
+  CHECK(((int64_t)c.batch * c.kv_heads * plan.splits + 8) * plan.tiles < (int64_t)1 << 31 && n * dims->n_heads < (int64_t)1 << 31,
         ACACHE_ERR_UNSUPPORTED);
   const PagedQueries r = {q, q_ld, out, out_ld, lse, key_len, rows_per_request, dims->n_heads};
   LAUNCH_T(ACACHE_K_ATTENTION, stream, launch_paged_attention(dims->dtype, c, r, plan, ws, stream));

@@ -82,6 +82,11 @@ __device__ __forceinline__ void dma16_asm(rsrc_words r, uint32_t voff, const cha
   const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)lds);
   asm volatile("buffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(r), "{m0}"(m0) : "memory");
 }
+// 16 bytes per lane from 64-bit addresses, global -> LDS at lds + 16 * lane.
+__device__ __forceinline__ void dma16_global_asm(const void* g, const char* lds) {
+  const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)lds);
+  asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(g), "{m0}"(m0) : "memory");
+}
 // 4 bytes per lane, buffer -> LDS at lds + 4 * lane.
 __device__ __forceinline__ void dma4_asm(rsrc_words r, uint32_t voff, const char* lds) {
   const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)lds);

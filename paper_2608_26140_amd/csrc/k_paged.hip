@@ -5,6 +5,7 @@
 // position past the table, or whose entry names no block of the pools, has no
 // slot: nothing is stored there, and it reads as a key and a value of zeros.
 #include <algorithm>
+#include <type_traits>
 
 #include "device.h"
 #include "internal.h"
@@ -14,6 +15,7 @@ namespace acache {
 namespace {
 
 typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
+typedef __attribute__((__vector_size__(2 * sizeof(uint16_t)))) uint16_t u16x2;
 
 // Slot of a request's position, -1 if it has none.
 __device__ __forceinline__ int slot_of(const PagedCache& c, const int32_t* __restrict__ table, int at) {
@@ -480,6 +482,231 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedCache c, P
   }
 }
 
+// Attention of 128 queries of a KV head, 32 to a wave, where there are that
+// many: tiles of 64 keys pass through LDS once for all four waves (two tiles, so
+// that one is copied while the other is read; a barrier a tile), and no two
+// waves' results have to be joined.  Blocks are of whole runs of 16 slots; a
+// wave copies one run of the tile, its pieces laid out so that the products'
+// fragments are read from distinct banks.
+//  - S^T = K Q^T on MFMA 32x32x16: a lane has query lane % 32 and, rows of K
+//    taken in the order of key_row, keys 16 (r / 8) + 8 (lane / 32) + r % 8 of
+//    each 32 in register r: what the second product wants of P;
+//  - O^T = V^T P^T, V's fragments by transposing reads.
+// Bound by its work: per tile and wave 32 products of 32 cycles, 32 exponentials
+// of 16 and some 200 other vector instructions, about half of what 32 queries
+// with keys of their own take (paged_attention_kernel).
+typedef __attribute__((__vector_size__(4 * sizeof(int16_t)))) int16_t i16x4;
+__device__ __forceinline__ i16x4 read_turned(const char* lds) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)lds);
+}
+__device__ __forceinline__ int key_row(int m) { return (m >> 4) * 16 + ((m >> 2) & 1) * 8 + ((m >> 3) & 1) * 4 + (m & 3); }
+__device__ __forceinline__ int v_swizzle(int row) { return ((row & 3) << 2) ^ (row & 1); }
+
+constexpr int kWideQueries = 128;
+__global__ __launch_bounds__(256, 2) void paged_attention_wide_kernel(PagedCache c, PagedQueries r, PagedPlan p) {
+  constexpr int TILE = 64, ROW = 256, HALF = TILE * ROW;
+  __shared__ __attribute__((aligned(1024))) char s_tile[2][2 * HALF];  // K, V
+  __shared__ int s_len[4];
+  Group gr;
+  if (!group_of(c, p, gr)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int qn = lane & 31, hl = lane >> 5, ln = lane & 15, lg = lane >> 4;
+  const int rep = r.heads / c.kv_heads, nq = r.per_request * rep;
+  const int q = gr.tile * kWideQueries + wave * 32 + qn;
+  const bool real = q < nq, live = gr.tile * kWideQueries + wave * 32 < nq;
+  const int qi = real ? q / rep : 0, h = gr.g * rep + (real ? q - qi * rep : 0);
+  const int64_t row = (int64_t)gr.b * r.per_request + qi;
+  const int klen = real ? capped_len(c, r.key_len[row]) : 0;
+  bf16x8 qf[8];
+#pragma unroll
+  for (int s = 0; s < 8; ++s)
+    qf[s] = *reinterpret_cast<const bf16x8*>((const bf16*)r.q + row * r.q_ld + h * 128 + s * 16 + hl * 8);
+  int longest = klen, shortest = real ? klen : 0x7FFFFFFF;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    longest = max(longest, __shfl_xor(longest, o));
+    shortest = min(shortest, __shfl_xor(shortest, o));
+  }
+  if (lane == 0) s_len[wave] = longest;
+  __syncthreads();
+  longest = max(max(s_len[0], s_len[1]), max(s_len[2], s_len[3]));
+  longest = __builtin_amdgcn_readfirstlane(longest);
+  shortest = __builtin_amdgcn_readfirstlane(shortest);
+
+  int begin, end;
+  share_of(longest, p.splits, gr.split, begin, end);
+  const int32_t* table = c.tables + (int64_t)gr.b * c.table_ld;
+  const float scale = kLog2e * 0.08838834764831845f;  // log2(e) / sqrt(128)
+
+  // copies: run `wave` of a tile, four rows an instruction
+  const uint32_t ld = (uint32_t)c.ld * 2u;
+  const char* kp = (const char*)c.k + gr.g * 256;
+  const char* vp = (const char*)c.v + gr.g * 256;
+  // (row i * 4 + lg of the run: the swizzles of its pieces are ln ^ lg ^ 4 i, and
+  // the same in every i)
+  const uint32_t k_piece = ln ^ lg, row_off = lg * ld, v_off = row_off + (ln ^ v_swizzle(lg)) * 16;
+  auto last_at = [&](int k) { return min(k, end - 1); };
+  auto block_at = [&](int k) { return table[(uint32_t)last_at(k) / (uint32_t)c.block]; };
+  int ahead = begin < end ? block_at(begin + wave * 16) : 0;
+  auto copy_tile = [&](int k0, int stage) {
+    const int at = (int)((uint32_t)last_at(k0 + wave * 16) % (uint32_t)c.block) & ~15;
+    const int id = __builtin_amdgcn_readfirstlane(ahead);
+    ahead = block_at(k0 + TILE + wave * 16);
+    char* to = s_tile[stage] + wave * 16 * ROW;
+    if (id >= 0 && id < c.n_blocks) {
+      const uint64_t from = (uint64_t)(uint32_t)(id * c.block + at) * ld;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        dma16_global_asm(kp + from + (uint64_t)(4 * i) * ld + (row_off + ((k_piece ^ (4 * i)) << 4)), to + i * 1024);
+        dma16_global_asm(vp + from + (uint64_t)(4 * i) * ld + v_off, to + HALF + i * 1024);
+      }
+    } else {  // keys without a slot are zeros
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<u32x4*>(to + i * 1024 + lane * 16) = *reinterpret_cast<u32x4*>(to + HALF + i * 1024 + lane * 16) =
+            u32x4{0, 0, 0, 0};
+    }
+  };
+
+  f32x16 acc[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
+  float m = -INFINITY, l = 0.f;
+  const int k_row = key_row(qn), v_row = 8 * (lg >> 1) + (ln >> 2), v_col = 2 * (lg & 1) + ((ln & 3) >> 1);
+  if (begin < end) copy_tile(begin, 0);
+  int stage = 0;
+  auto take = [&](auto masked, int k0) {
+    wait_vmcnt<0>();
+    wait_lgkmcnt<0>();
+    bare_barrier();  // the tile is there, and nobody reads the other one
+    if (k0 + TILE < end) copy_tile(k0 + TILE, stage ^ 1);
+    const char* kt = s_tile[stage];
+    const char* vt = kt + HALF;
+    stage ^= 1;
+    if (!live) return;
+    f32x16 s[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
+#pragma unroll
+    for (int st = 0; st < 8; ++st)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + (kb * 32 + k_row) * ROW + (((2 * st + hl) ^ (k_row & 15)) << 4));
+        s[kb] = mfma32x32x16(kf, qf[st], s[kb]);
+      }
+    if constexpr (masked.value)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          s[kb][i] = k0 + kb * 32 + 16 * (i >> 3) + 8 * hl + (i & 7) < klen ? s[kb][i] : -INFINITY;
+    float top = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+    top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+    if (__ballot(top > m)) {
+      const bool up = top > m;
+      const float f = up ? __builtin_amdgcn_exp2f((m - top) * scale) : 1.f;
+      l *= f;
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] *= f;
+      m = up ? top : m;
+    }
+    const float from = m == -INFINITY ? 0.f : m * scale;
+    bf16x8 pf[4];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float w = __builtin_amdgcn_exp2f(fmaf(s[kb][i], scale, -from));
+        s[kb][i] = w;
+        l += w;
+        pf[kb * 2 + (i >> 3)][i & 7] = (bf16)w;
+      }
+    u16x2 least = {1, 1};  // 0: an infinity or NaN of V where some query does not attend (see above)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          const char* at = vt + (g * 16 + v_row) * ROW + (((4 * d + v_col) ^ v_swizzle(v_row)) << 4) + (ln & 1) * 8;
+          const i16x4 lo = read_turned(at), hi = read_turned(at + 4 * ROW);
+          u32x4 vf = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+          if constexpr (masked.value)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {  // both halves at a time: 0 where the exponent is all ones
+              const uint32_t word = vf[w];
+              const u16x2 y = __builtin_bit_cast(u16x2, word);
+              const u16x2 rest = __builtin_elementwise_min((y & (u16x2){0x7F80, 0x7F80}) ^ (u16x2){0x7F80, 0x7F80}, (u16x2){1, 1});
+              least = __builtin_elementwise_min(least, rest);
+              vf[w] = __builtin_bit_cast(uint32_t, y & ((u16x2){0, 0} - rest));
+            }
+          acc[d] = mfma32x32x16(__builtin_bit_cast(bf16x8, vf), pf[g], acc[d]);
+        }
+    if constexpr (masked.value)
+      if (__ballot((least[0] & least[1]) == 0)) {
+#pragma unroll 1
+      for (int key = 0; key < TILE; ++key) {
+        float w = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (key >> 5 == kb && ((key >> 4) & 1) * 8 + (key & 7) == i) w = s[kb][i];
+        w = (float)(bf16)__shfl(w, qn + ((key >> 3) & 1) * 32);
+        const bool seen = k0 + key < klen;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int e = d * 32 + 8 * (i >> 2) + 4 * hl + (i & 3);
+            const bf16 x = *reinterpret_cast<const bf16*>(vt + key * ROW + (((e >> 3) ^ v_swizzle(key)) << 4) + (e & 7) * 2);
+            const float v = to_f32(x);
+            if (seen && !(fabsf(v) < INFINITY)) acc[d][i] += w * v;
+          }
+      }
+    }
+  };
+  // tiles that all of the wave's queries attend to whole, then the others
+  int k0 = begin;
+  for (; k0 < end && k0 + TILE <= shortest; k0 += TILE) take(std::false_type{}, k0);
+  for (; k0 < end; k0 += TILE) take(std::true_type{}, k0);
+
+  if (!real) return;
+  const float total = l + __shfl_xor(l, 32);
+  if (p.splits == 1) {
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    bf16* dst = (bf16*)r.out + row * r.out_ld + h * 128 + 4 * hl;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        bf16x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (bf16)(acc[d][i + e] * inv);
+        *reinterpret_cast<bf16x4*>(dst + d * 32 + 2 * i) = v;
+      }
+    if (r.lse && hl == 0) r.lse[row * r.heads + h] = ((m == -INFINITY ? 0.f : m * scale) + __builtin_amdgcn_logf(total)) * kLn2;
+  } else {
+    const int64_t at = ((int64_t)gr.split * c.batch * r.per_request + row) * r.heads + h;
+    float* dst = p.part + at * 128 + 4 * hl;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *reinterpret_cast<f32x4*>(dst + d * 32 + 2 * i) = f32x4{acc[d][i], acc[d][i + 1], acc[d][i + 2], acc[d][i + 3]};
+    if (hl == 0) p.stats[at] = make_float2(m * scale, total);
+  }
+}
+
 // fp32: 16 lanes share a key (elements lane % 16 + 16 i), a wave four keys at a
 // time, four such on their way; every 16 lanes keep a running softmax of their
 // own for the tile's four queries.
@@ -669,7 +896,18 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedCache c, PagedQue
   if (r.lse && lane == 0) r.lse[at] = (from + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
-int tile_queries(int queries, bool f32) { return f32 ? kQueriesF32 : queries <= 16 ? 16 : 32; }
+// Blocks are of whole runs of 16 slots, 16 rows of which lie within 2^31 bytes.
+bool in_runs(const PagedCache& c) { return c.block % 16 == 0 && c.ld < 1 << 26; }
+
+// Tiles of 128 from 193 queries on, where both of a KV head's first two are more
+// than half full: 4 x 32 rows of 28 heads on 4 (224 queries) over 5120 keys 28 us,
+// 32 with tiles of 32; 4 x 256 rows (1792) over 4096 keys 98, 122; but 160
+// queries of one KV head over 3000 keys 15.3, 13.4.
+int tile_queries(int queries, bool f32, bool runs) {
+  if (f32) return kQueriesF32;
+  if (runs && queries > 192) return kWideQueries;
+  return queries <= 16 ? 16 : 32;
+}
 
 }  // namespace
 
@@ -694,7 +932,7 @@ PagedPlan plan_paged_attention(acache_dtype dt, const PagedCache& c, int per_req
                                size_t ws_bytes) {
   PagedPlan p = {};
   const int queries = per_request * (heads / c.kv_heads);
-  p.tile = tile_queries(queries, dt == ACACHE_F32);
+  p.tile = tile_queries(queries, dt == ACACHE_F32, in_runs(c));
   p.tiles = (queries + p.tile - 1) / p.tile;
   const int64_t groups = (int64_t)c.batch * c.kv_heads * p.tiles;
   const int64_t pairs = (int64_t)c.batch * per_request * heads;
@@ -705,11 +943,12 @@ PagedPlan plan_paged_attention(acache_dtype dt, const PagedCache& c, int per_req
   // chain of dependent waits that grows with the load, the rate of the memory for
   // all that run (6 TB/s; tiles of the same keys read them once), and the work of
   // those that share a CU.  The join is a launch, and the partials' way.  One row
-  // of 8 requests over 30011 keys, 4 KV heads: 323 us unsplit, 99 in 5 parts, 85
-  // in 8, 84 in 16, 92 in 32; 4 x 32 rows of 28 heads over 5120 keys: 48, 2 parts
-  // 34, 4 parts 30, 8 parts 34.
-  const bool wide = p.tile == 32, f32 = dt == ACACHE_F32;
-  const double chain = f32 ? 2.0 : wide ? 1.1 : 1.3, work = f32 ? 1.5 : wide ? 1.05 : 0.6;
+  // of 8 requests over 30011 keys, 4 KV heads: 321 us unsplit, 96 in 5 parts, 85
+  // in 8, 84 in 16, 92 in 32; 4 x 32 rows of 28 heads over 5120 keys: 108, 2 parts
+  // 64, 4 parts 39, 8 parts 28, 16 parts 34.
+  const bool f32 = dt == ACACHE_F32;
+  const double chain = f32 ? 2.0 : p.tile == kWideQueries ? 2.6 : p.tile == 32 ? 1.1 : 1.3;
+  const double work = f32 ? 1.5 : p.tile == kWideQueries ? 2.8 : p.tile == 32 ? 1.05 : 0.6;
   int64_t splits = 1;
   double best = 1e30;
   for (int64_t s = 1; s <= std::max<int64_t>(most, 1); ++s) {
@@ -737,14 +976,15 @@ hipError_t launch_paged_attention(acache_dtype dt, const PagedCache& c, const Pa
   p.stats = (float2*)(p.part + pairs * p.splits * c.head_dim);
   const int64_t keys = (int64_t)c.batch * c.kv_heads * p.splits;
   const dim3 grid((unsigned)((keys + 7) / 8 * 8 * p.tiles));
-  const bool runs = c.block % 16 == 0 && c.ld < 1 << 26;  // 16 rows within 2^31 bytes
+  const bool runs = in_runs(c);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, c, r, p); };
   if (dt == ACACHE_F32) {
     if (c.head_dim <= 32) go(paged_attention_f32_kernel<2>);
     else if (c.head_dim <= 64) go(paged_attention_f32_kernel<4>);
     else go(paged_attention_f32_kernel<8>);
   } else {
-    if (p.tile == 16) runs ? go(paged_attention_kernel<1, true>) : go(paged_attention_kernel<1, false>);
+    if (p.tile == kWideQueries) go(paged_attention_wide_kernel);
+    else if (p.tile == 16) runs ? go(paged_attention_kernel<1, true>) : go(paged_attention_kernel<1, false>);
     else runs ? go(paged_attention_kernel<2, true>) : go(paged_attention_kernel<2, false>);
   }
   if (p.splits > 1) {

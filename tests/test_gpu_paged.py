@@ -191,6 +191,46 @@ def test_rows(dt, H, G, d, per, causal):
     run_attention(dt, H, G, d, 3, per, 16, lens, strided=True)
 
 
+@pytest.mark.parametrize("H,G,per", [(28, 4, 10), (28, 4, 32), (8, 1, 17), (4, 4, 130), (28, 4, 19)])
+@pytest.mark.parametrize("block,causal", [(16, True), (64, False), (48, True)])
+def test_many_rows(H, G, per, block, causal):
+    """Tiles of 32 and of 128 queries: whole ones and parts of one, waves without any."""
+    print(f"many rows {H}/{G}, {per} rows, block {block}, causal {causal}", flush=True)
+    lens = [n - (per - 1 - i) if causal else n for n in (max(per, 200), max(per, 333)) for i in range(per)]
+    run_attention(BF, H, G, 128, 2, per, block, lens, strided=True)
+
+
+@pytest.mark.parametrize("per", [25, 40])
+def test_many_rows_of_any_lengths(per):
+    g = torch.Generator().manual_seed(16)
+    lens = torch.randint(0, 300, (3 * per,), generator=g)
+    lens[::7] = 0
+    lens[per:2 * per] = 0
+    run_attention(BF, 28, 4, 128, 3, per, 32, lens.tolist())
+
+
+@pytest.mark.parametrize("per", [20, 32])
+@pytest.mark.parametrize("ws", ["none", 3, "all"])
+def test_many_rows_split(ws, per):
+    run_attention(BF, 28, 4, 128, 1, per, 16, [1500 + i for i in range(per)], ws=ws)
+
+
+@pytest.mark.parametrize("per", [20, 30])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_odd_numbers_beside_many_rows(bad, per):
+    """As below, with tiles of 32 and of 128 queries, entries without a block among them."""
+    H, G, d = 28, 4, 128
+    tables = torch.tensor([[6, 2, -1, 0, 3, 7, 1, 99]], dtype=torch.int32)
+    lens = [100 + i % 20 for i in range(per)]
+    lens[4], lens[9] = 3, 0
+    kp, vp = pools(8 * 16, G * d, BF, seed=21)
+    vp[R.slot(tables, 8, 16, 0, 110), 1] = bad
+    vp[R.slot(tables, 8, 16, 0, 105), G * d - 1] = bad
+    vp[R.slot(tables, 8, 16, 0, 50), 7] = bad
+    kp[R.slot(tables, 8, 16, 0, 109), :d] = bad
+    run_attention(BF, H, G, d, 1, per, 16, lens, tables=tables, kv=(kp, vp), poison=False)
+
+
 @pytest.mark.parametrize("dt,H,G,d", [SHAPES[1], SHAPES[3]])
 def test_rows_of_any_lengths(dt, H, G, d):
     """Every row a length of its own, empty ones and negative ones among them."""
