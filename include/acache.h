@@ -605,7 +605,7 @@ typedef struct {
  * rotated on half-split pairs by pos[m] * theta_i, as acache_layer_recompute
  * rotates, and goes with row m of v to the slot of position at[m] (at NULL:
  * pos[m]).  With q (nullable) its rows are rotated likewise into q_out (which
- * may be q itself).  A row with pos[m] < 0 is padding: nothing of it is stored
+ * may be q itself, with the same stride).  A row with pos[m] < 0 is padding: nothing of it is stored
  * and its row of q_out is zeros.  A row whose position has no slot is rotated
  * but not stored.  Rows of one call name different slots (of two that name one,
  * elements of either are stored).  Slots that no row names keep every bit.
@@ -613,7 +613,7 @@ typedef struct {
  *   k [rows, k_ld], v [rows, v_ld]: H_kv * head_dim; rows = batch * rows_per_request
  * A projection's fused rows serve as q, k and v with one stride.  The sources
  * must not overlap the pools.  bf16: pointers and strides are multiples of 16
- * bytes.  rows == 0: no-op. */
+ * bytes.  rows < 2^24.  rows == 0: no-op. */
 acache_status acache_paged_append(const acache_dims* dims, const acache_paged_cache* cache, int32_t rows_per_request,
                                   const void* q, int64_t q_ld, const void* k, int64_t k_ld, const void* v, int64_t v_ld,
                                   const int32_t* pos, const int32_t* at, void* q_out, int64_t q_out_ld,
@@ -637,7 +637,9 @@ acache_status acache_paged_append(const acache_dims* dims, const acache_paged_ca
  * tables' capacity); it sets how the keys are split over workgroups and nothing
  * else.  ws is optional: with acache_paged_workspace_size() bytes calls with
  * few rows split the keys (fp32 partials, joined in a fixed order); with less,
- * in fewer parts or none.  rows < 2^30 and rows * H < 2^31.  rows == 0: no-op. */
+ * in fewer parts or none.  rows and batch * H_kv * (rows_per_request * H / H_kv / 16,
+ * f32 4, rounded up) are below 2^24 (ACACHE_ERR_UNSUPPORTED otherwise).  rows == 0:
+ * no-op. */
 acache_status acache_paged_attention(const acache_dims* dims, const acache_paged_cache* cache, int32_t rows_per_request,
                                      const void* q, int64_t q_ld, const int32_t* key_len, int64_t max_len, void* out,
                                      int64_t out_ld, float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
@@ -677,8 +679,8 @@ acache_status acache_paged_attention_schedule(const acache_dims* dims, const aca
  *   prob (nullable) fp32 [rows]: the probability it was drawn with (greedy: 1)
  * commit_pos, ids: as in acache_argmax_commit.  Weights are summed as integers
  * (2^-44 of the largest is 1), so the result does not depend on the order of
- * the work.  n <= 2^19 (ACACHE_ERR_UNSUPPORTED otherwise).  rows == 0: no-op;
- * n == 0 with rows > 0: ACACHE_ERR_SHAPE. */
+ * the work.  n <= 2^19 and rows < 2^22 (ACACHE_ERR_UNSUPPORTED otherwise).
+ * rows == 0: no-op; n == 0 with rows > 0: ACACHE_ERR_SHAPE. */
 acache_status acache_sample_commit(acache_dtype dtype, const void* x, int64_t ld, int32_t rows, int32_t n,
                                    const float* temperature, const int32_t* top_k, const float* top_p,
                                    const float* min_p, const double* u, int32_t* out, float* conf, float* prob,

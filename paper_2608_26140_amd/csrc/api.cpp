@@ -1165,7 +1165,8 @@ acache_status check_paged(const acache_dims* d, const acache_paged_cache* c, int
   CHECK(c->ld < k31 / 2, ACACHE_ERR_UNSUPPORTED);
   CHECK(c->n_blocks < k31 && c->n_blocks * c->block < k31 && (int64_t)c->max_blocks * c->block < k31 / 2,
         ACACHE_ERR_UNSUPPORTED);
-  CHECK((int64_t)c->batch * rows_per_request < k31 / 2, ACACHE_ERR_UNSUPPORTED);
+  // a launch has less than 2^24 workgroups of 256 threads
+  CHECK((int64_t)c->batch * rows_per_request < 1 << 24, ACACHE_ERR_UNSUPPORTED);
   out = PagedCache{c->k, c->v, c->ld, (int)c->n_blocks, c->block, d->n_kv_heads, d->head_dim, c->tables, c->table_ld,
                    c->batch, c->max_blocks};
   return ACACHE_OK;
@@ -1200,6 +1201,7 @@ acache_status acache_paged_append(const acache_dims* dims, const acache_paged_ca
   const bool rows16 = aligned_rows(c.k, c.ld, es) && aligned_rows(c.v, c.ld, es) && aligned_rows(k, k_ld, es) &&
                       aligned_rows(v, v_ld, es) && (!q || (aligned_rows(q, q_ld, es) && aligned_rows(q_out, q_out_ld, es)));
   CHECK(dims->dtype == ACACHE_F32 || rows16, ACACHE_ERR_ALIGN);
+  CHECK(!q || q != q_out || q_ld == q_out_ld, ACACHE_ERR_SHAPE);
   const AppendRows r = {q, k, v, q_out, q_ld, k_ld, v_ld, q_out_ld, pos, at, (int)n, rows_per_request, dims->n_heads,
                         rows16 && dims->head_dim % 8 == 0};
   LAUNCH_T(ACACHE_K_SCATTER, stream, launch_paged_append(dims->dtype, c, r, dims->rope_base, stream));
@@ -1224,9 +1226,7 @@ acache_status acache_paged_attention(const acache_dims* dims, const acache_paged
           ACACHE_ERR_ALIGN);
   CHECK(!ws || aligned16(ws), ACACHE_ERR_ALIGN);
   const PagedPlan plan = plan_paged(dims, c, rows_per_request, max_len, ws ? ws_bytes : 0);
-  // one dimension of workgroups, in the join one for a (row, head) pair
-  CHECK(((int64_t)c.batch * c.kv_heads * plan.splits + 8) * plan.tiles < (int64_t)1 << 31 && n * dims->n_heads < (int64_t)1 << 31,
-        ACACHE_ERR_UNSUPPORTED);
+  CHECK((int64_t)c.batch * c.kv_heads * plan.splits * plan.tiles < (1 << 24) - 8 * (int64_t)plan.tiles, ACACHE_ERR_UNSUPPORTED);
   const PagedQueries r = {q, q_ld, out, out_ld, lse, key_len, rows_per_request, dims->n_heads};
   LAUNCH_T(ACACHE_K_ATTENTION, stream, launch_paged_attention(dims->dtype, c, r, plan, ws, stream));
   return ACACHE_OK;
@@ -1258,7 +1258,7 @@ acache_status acache_sample_commit(acache_dtype dtype, const void* x, int64_t ld
   CHECK(rows >= 0 && n >= 0 && ld >= n && ids_len >= 0, ACACHE_ERR_SHAPE);
   if (rows == 0) return ACACHE_OK;
   CHECK(n > 0, ACACHE_ERR_SHAPE);
-  CHECK(n <= 1 << 19, ACACHE_ERR_UNSUPPORTED);
+  CHECK(n <= 1 << 19 && rows < 1 << 22, ACACHE_ERR_UNSUPPORTED);
   CHECK(x && u && out && (!commit_pos || ids), ACACHE_ERR_NULL);
   const SampleRows r = {x, ld, n, temperature, top_p, min_p, top_k, u, out, conf, prob, commit_pos, ids, ids_len};
   LAUNCH_T(ACACHE_K_ARGMAX, stream, launch_sample_commit(dtype, r, rows, stream));

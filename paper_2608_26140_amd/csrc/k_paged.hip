@@ -33,62 +33,57 @@ struct Run {  // V consecutive elements of one half of a head
 
 // Rows of K and Q are turned by pos * theta_i, theta_i = base^(-2i/d), in each
 // half-split pair (i, i + d/2); rows of V are copied.  An item is V pairs of
-// one head: two runs of V elements, in and out.  A workgroup takes `rows` rows
-// and the items [blockIdx.y, + gridDim.y, ..) of each; it evaluates every
-// angle of its rows once (fp64, rotary_sincos) into LDS while its first items
-// are on their way.  Bound by memory: each element is read and written once.
+// one head: two runs of V elements, in and out.  A workgroup takes the items
+// [256 blockIdx.y, + 256 gridDim.y, ..) of a row, whose angles it evaluates once
+// (fp64, rotary_sincos) into LDS.  Bound by memory: each element is read and
+// written once (8192 rows of 32 + 64 heads of 128 bf16, 403 MB: 77 us, 5.2 TB/s).
 template <typename T, int V>
-__global__ __launch_bounds__(256) void paged_append_kernel(PagedCache c, AppendRows r, int rows, double log2_base) {
-  extern __shared__ float2 turn[];  // [rows][half]: cos, sin
+__global__ __launch_bounds__(256) void paged_append_kernel(PagedCache c, AppendRows r, double log2_base) {
+  extern __shared__ float2 turn[];  // [half]: cos, sin
   const int half = c.head_dim >> 1, per_head = half / V;
   const int heads = (r.q ? r.heads : 0) + 2 * c.kv_heads;
   const int items = heads * per_head;
-  const int first = blockIdx.x * rows;
-  const int here = min(rows, r.n - first);
-  for (int t = threadIdx.x; t < here * half; t += 256) {
-    const int row = t / half, i = t - row * half;
+  const int m = blockIdx.x, b = m / r.per_request, pos = r.pos[m];
+  for (int i = threadIdx.x; i < half; i += 256) {
     float sn = 0.f, cs = 0.f;
-    rotary_sincos((double)r.pos[first + row] * exp2(-(2.0 * i / c.head_dim) * log2_base), &sn, &cs);
-    turn[t] = make_float2(cs, sn);
+    rotary_sincos((double)pos * exp2(-(2.0 * i / c.head_dim) * log2_base), &sn, &cs);
+    turn[i] = make_float2(cs, sn);
   }
   __syncthreads();
-  for (int row = 0; row < here; ++row) {
-    const int m = first + row, b = m / r.per_request, pos = r.pos[m];
-    const int64_t slot = pos < 0 ? -1 : slot_of(c, c.tables + (int64_t)b * c.table_ld, r.at ? r.at[m] : pos);
-    for (int t = blockIdx.y * 256 + threadIdx.x; t < items; t += gridDim.y * 256) {
-      int h = t / per_head;
-      const int i = (t - h * per_head) * V;
-      const T* src;
-      T* dst;
-      bool turned = true;
-      if (h < heads - 2 * c.kv_heads) {
-        src = (const T*)r.q + (int64_t)m * r.q_ld + h * c.head_dim;
-        dst = (T*)r.q_out + (int64_t)m * r.q_out_ld + h * c.head_dim;
-      } else {
-        if (slot < 0) continue;
-        h -= heads - 2 * c.kv_heads;
-        turned = h < c.kv_heads;
-        if (!turned) h -= c.kv_heads;
-        src = turned ? (const T*)r.k + (int64_t)m * r.k_ld : (const T*)r.v + (int64_t)m * r.v_ld;
-        dst = (T*)(turned ? c.k : c.v) + slot * c.ld;
-        src += h * c.head_dim;
-        dst += h * c.head_dim;
-      }
-      Run<T, V> lo, hi;
-      __builtin_memcpy(&lo, src + i, sizeof(lo));
-      __builtin_memcpy(&hi, src + i + half, sizeof(hi));
-      if (turned) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const float2 a = pos < 0 ? make_float2(0.f, 0.f) : turn[row * half + i + j];
-          const float x = to_f32(lo.e[j]), y = to_f32(hi.e[j]);
-          lo.e[j] = from_f32<T>(pos < 0 ? 0.f : x * a.x - y * a.y);
-          hi.e[j] = from_f32<T>(pos < 0 ? 0.f : y * a.x + x * a.y);
-        }
-      }
-      __builtin_memcpy(dst + i, &lo, sizeof(lo));
-      __builtin_memcpy(dst + i + half, &hi, sizeof(hi));
+  const int64_t slot = pos < 0 ? -1 : slot_of(c, c.tables + (int64_t)b * c.table_ld, r.at ? r.at[m] : pos);
+  for (int t = blockIdx.y * 256 + threadIdx.x; t < items; t += gridDim.y * 256) {
+    int h = t / per_head;
+    const int i = (t - h * per_head) * V;
+    const T* src;
+    T* dst;
+    bool turned = true;
+    if (h < heads - 2 * c.kv_heads) {
+      src = (const T*)r.q + (int64_t)m * r.q_ld + h * c.head_dim;
+      dst = (T*)r.q_out + (int64_t)m * r.q_out_ld + h * c.head_dim;
+    } else {
+      if (slot < 0) continue;
+      h -= heads - 2 * c.kv_heads;
+      turned = h < c.kv_heads;
+      if (!turned) h -= c.kv_heads;
+      src = turned ? (const T*)r.k + (int64_t)m * r.k_ld : (const T*)r.v + (int64_t)m * r.v_ld;
+      dst = (T*)(turned ? c.k : c.v) + slot * c.ld;
+      src += h * c.head_dim;
+      dst += h * c.head_dim;
     }
+    Run<T, V> lo, hi;
+    __builtin_memcpy(&lo, src + i, sizeof(lo));
+    __builtin_memcpy(&hi, src + i + half, sizeof(hi));
+    if (turned) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float2 a = pos < 0 ? make_float2(0.f, 0.f) : turn[i + j];
+        const float x = to_f32(lo.e[j]), y = to_f32(hi.e[j]);
+        lo.e[j] = from_f32<T>(pos < 0 ? 0.f : x * a.x - y * a.y);
+        hi.e[j] = from_f32<T>(pos < 0 ? 0.f : y * a.x + x * a.y);
+      }
+    }
+    __builtin_memcpy(dst + i, &lo, sizeof(lo));
+    __builtin_memcpy(dst + i + half, &hi, sizeof(hi));
   }
 }
 
@@ -164,10 +159,11 @@ __device__ __forceinline__ float most_of_four(float v) {
 // weight is 1, which rounding leaves as it is: raising it only in steps of 2^8
 // saves 6% with 224 queries of a KV head, and takes the error against 64 bits
 // from 0.0019 to 0.0026.
-// RUNS: blocks are of whole runs of 16 slots, so that the 16 keys of a tile lie
-// one behind the other: their rows are a scalar base and per-lane offsets that
-// do not change.  Otherwise every lane finds the slot of one key and the others
-// get it from there (a third of the step's vector instructions).
+// Every lane finds the slot of one key and the others get it from there.  RUNS:
+// blocks are of whole runs of 16 slots, so that the 16 keys of a tile lie one
+// behind the other: their rows are a scalar base and per-lane offsets that do not
+// change (2 x 16 rows of 28 heads on 4 over 8192 keys 20.9 us, 22.1 without; with
+// one tile of queries, 32 requests or 1 over 1537 to 30011 keys, no difference).
 template <int QT, bool RUNS>
 __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedCache c, PagedQueries r, PagedPlan p) {
   constexpr int LDO = 132;  // padded rows of the exchange
@@ -899,6 +895,8 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedCache c, PagedQue
 // Blocks are of whole runs of 16 slots, 16 rows of which lie within 2^31 bytes.
 bool in_runs(const PagedCache& c) { return c.block % 16 == 0 && c.ld < 1 << 26; }
 
+// Tiles of 16 for up to 16 queries: 7 of each of 4 KV heads of 8 requests over 8192
+// keys 31.3 us, 33.7 with tiles of 32; 28 of each 47.9, 37.1.
 // Tiles of 128 from 193 queries on, where both of a KV head's first two are more
 // than half full: 4 x 32 rows of 28 heads on 4 (224 queries) over 5120 keys 28 us,
 // 32 with tiles of 32; 4 x 256 rows (1792) over 4096 keys 98, 122; but 160
@@ -914,13 +912,12 @@ int tile_queries(int queries, bool f32, bool runs) {
 hipError_t launch_paged_append(acache_dtype dt, const PagedCache& c, const AppendRows& r, float rope_base, hipStream_t s) {
   const double l2b = log2((double)rope_base);
   const int half = c.head_dim / 2, heads = (r.q ? r.heads : 0) + 2 * c.kv_heads;
-  // a few rows: one to a workgroup, its items spread over several
-  const int rows = r.n >= 2048 ? 4 : 1;
+  // Below 1024 rows a row's items are spread over workgroups, each with all of its
+  // angles: 512 rows of 28 + 8 heads 4.3 us, 7.7 with several rows to a workgroup;
+  // from there on one takes them all: 1024 rows 6.3, spread 7.2, 8192 rows 30.5, 40.
   auto go = [&](auto kernel, int v) {
-    const int items = heads * (half / v);
-    const int parts = rows > 1 ? 1 : std::min(64, (items + 255) / 256);
-    hipLaunchKernelGGL(kernel, dim3((r.n + rows - 1) / rows, parts), dim3(256), (size_t)rows * half * sizeof(float2), s, c,
-                       r, rows, l2b);
+    const int parts = r.n >= 1024 ? 1 : std::min(64, (heads * (half / v) + 255) / 256);
+    hipLaunchKernelGGL(kernel, dim3(r.n, parts), dim3(256), (size_t)half * sizeof(float2), s, c, r, l2b);
   };
   if (dt == ACACHE_BF16) go(paged_append_kernel<bf16, 8>, 8);
   else if (r.vec) go(paged_append_kernel<float, 4>, 4);
@@ -937,7 +934,11 @@ PagedPlan plan_paged_attention(acache_dtype dt, const PagedCache& c, int per_req
   const int64_t groups = (int64_t)c.batch * c.kv_heads * p.tiles;
   const int64_t pairs = (int64_t)c.batch * per_request * heads;
   const size_t each = (size_t)pairs * (c.head_dim + 2) * sizeof(float);
-  const int64_t most = std::min<int64_t>({(max_len + 127) / 128, kMaxSplits, (int64_t)(ws_bytes / std::max<size_t>(each, 1))});
+  // a launch has less than 2^24 workgroups of 256 threads
+  constexpr int64_t kMost = 1 << 24;
+  const int64_t most = pairs >= kMost ? 1
+                                      : std::min<int64_t>({(max_len + 127) / 128, kMaxSplits, (kMost - 8) / groups,
+                                                           (int64_t)(ws_bytes / std::max<size_t>(each, 1))});
   // The split with the least estimated time, in us.  Workgroups run two a CU, in
   // rounds; one takes a step for every 128 keys.  A step is the longest of a
   // chain of dependent waits that grows with the load, the rate of the memory for
@@ -976,19 +977,21 @@ hipError_t launch_paged_attention(acache_dtype dt, const PagedCache& c, const Pa
   p.stats = (float2*)(p.part + pairs * p.splits * c.head_dim);
   const int64_t keys = (int64_t)c.batch * c.kv_heads * p.splits;
   const dim3 grid((unsigned)((keys + 7) / 8 * 8 * p.tiles));
-  const bool runs = in_runs(c);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, c, r, p); };
   if (dt == ACACHE_F32) {
+    // 16 requests of 5 rows, 8 heads of 32 on 4, over 4096 keys: 60 us, 107 with the
+    // elements of a head of 128; heads of 64: 84, 119
     if (c.head_dim <= 32) go(paged_attention_f32_kernel<2>);
     else if (c.head_dim <= 64) go(paged_attention_f32_kernel<4>);
     else go(paged_attention_f32_kernel<8>);
   } else {
     if (p.tile == kWideQueries) go(paged_attention_wide_kernel);
-    else if (p.tile == 16) runs ? go(paged_attention_kernel<1, true>) : go(paged_attention_kernel<1, false>);
-    else runs ? go(paged_attention_kernel<2, true>) : go(paged_attention_kernel<2, false>);
+    else if (p.tile == 16) go(paged_attention_kernel<1, false>);
+    else in_runs(c) ? go(paged_attention_kernel<2, true>) : go(paged_attention_kernel<2, false>);
   }
   if (p.splits > 1) {
-    // one wave a pair with few splits, else four
+    // one wave a pair with up to 8 splits (4 x 32 rows of 28 heads in 8: 27.5 us,
+    // 33.4 with four waves), else four (one row of 32 heads in 13: 11.9, 12.7)
     const dim3 few((unsigned)((pairs + 3) / 4)), many((unsigned)pairs);
     if (dt == ACACHE_F32 && p.splits <= 8) hipLaunchKernelGGL((paged_merge_kernel<float, 1>), few, dim3(256), 0, s, c, r, p);
     else if (dt == ACACHE_F32) hipLaunchKernelGGL((paged_merge_kernel<float, 4>), many, dim3(256), 0, s, c, r, p);

@@ -40,6 +40,7 @@ def test_cache_checks(call):
     assert call(c=cache(n_blocks=1 << 27)) == 4                # 2^31 slots
     assert call(c=cache(max_blocks=1 << 27, table_ld=1 << 27)) == 4
     assert call(c=cache(batch=1 << 20), per=1 << 10) == 4
+    assert call(c=cache(batch=1 << 20), per=16) == 4           # 2^24 rows
     assert call(c=cache(k=None)) == 1 and call(c=cache(v=None)) == 1 and call(c=cache(tables=None)) == 1
     assert call(c=cache(k=264)) == 3 and call(c=cache(ld=260)) == 3
     assert call(d=dims(d=64)) == 4                             # bf16 heads are of 128
@@ -50,12 +51,14 @@ def test_append_checks():
     assert append(k=None) == 1 and append(v=None) == 1 and append(pos=None) == 1
     assert append(q_out=None) == 1
     assert append(k_ld=128) == 2 and append(v_ld=128) == 2 and append(q_ld=1016) == 2 and append(q_out_ld=1016) == 2
+    assert append(q_ld=1032) == 2                              # q_out is q, with another stride
     assert append(q=ctypes.c_void_p(264)) == 3 and append(k_ld=260) == 3 and append(q_out_ld=1028) == 3
 
 
 def test_attention_checks():
     assert attention(q=None) == 1 and attention(out=None) == 1 and attention(key_len=None) == 1
     assert attention(q_ld=1016) == 2 and attention(out_ld=1000) == 2
+    assert attention(c=cache(batch=1 << 20), d=dims("f32"), per=8) == 4  # 2^24 tiles of four queries
     assert attention(out=ctypes.c_void_p(260)) == 3 and attention(ws=ctypes.c_void_p(260), ws_bytes=1 << 20) == 3
 
 
@@ -65,7 +68,7 @@ def test_sample_checks():
                                           ids_len, None)
     assert call(dtype=7) == 4
     assert call(rows=-1) == 2 and call(n=-1) == 2 and call(ld=99) == 2 and call(ids_len=-1) == 2 and call(n=0, ld=0) == 2
-    assert call(n=(1 << 19) + 1, ld=1 << 20) == 4
+    assert call(n=(1 << 19) + 1, ld=1 << 20) == 4 and call(rows=1 << 22) == 4
     assert call(x=None) == 1 and call(u=None) == 1 and call(out=None) == 1 and call(pos=P) == 1
     assert call(rows=0) == 0
 
