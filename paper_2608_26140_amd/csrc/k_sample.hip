@@ -12,14 +12,18 @@
 // where u falls within about n 2^-44 of the row's weight of a border.
 //
 // The kernels take a row as a histogram over the upper 16 bits of its logits,
-// one bin for each such value of magnitude 2^-27 to 512 and one for 0, in LDS.
-// Of bf16 logits a bin's tokens are equal: its weight is its count times one
-// exponential, and a border in the bin is a division.  Of fp32 logits a bin
-// sums its tokens' weights, and a border is then looked for among its tokens.
-// Rows with other logits that carry weight (512 and more; below 2^-27 and not
-// 0), and fp32 rows with more than 1024 tokens of several values in a border's
-// bin, go by sample_any, which refines a histogram over the logits' order keys
-// and reads the row anew for each step.
+// one bin for each such value of magnitude 2^-27 to 512 and one for what lies
+// between, mostly zeros, in LDS.  Of bf16 logits a bin's tokens are equal: its
+// weight is its count times one exponential, and a border in the bin is a
+// division.  Of fp32 logits a bin sums its tokens' weights, and a border is then
+// looked for among its tokens.  Rows with logits of 512 and more, with a border
+// among the smallest ones when they are not all zeros, bf16 rows with more than
+// kSmall nonzero ones of these, and fp32 rows with more than 1024 tokens of
+// several values in a border's bin go by sample_any, which refines a histogram
+// over the logits' order keys and reads the row anew for each step (a call of
+// 1024 rows of 126464 takes 720 us with one such row, 77 without; of normally
+// distributed logits some 10^-9 are nonzero and below 2^-27, which is why these
+// have a place of their own).
 #include "device.h"
 #include "internal.h"
 
@@ -381,8 +385,8 @@ constexpr int kGroups = (kValues + 127) / 128;             // of 128 bins, two a
 constexpr int kBins = kGroups * 128;
 static_assert(kGroups <= 128, "two groups a lane");
 
-// Bins are numbered in the order of the values, largest first, zeros are bin
-// kRange; in memory the positive ones lie in ascending order.
+// Bins are numbered in the order of the values, largest first, zeros and what is
+// below 2^-27 are bin kRange; in memory the positive ones lie in ascending order.
 __device__ __forceinline__ int place_of(int bin) { return bin < kRange ? kRange - 1 - bin : bin; }
 __device__ __forceinline__ uint32_t half_of_bin(int bin) {
   const uint32_t off = bin < kRange ? kRange - 1 - bin : bin - kRange - 1;
@@ -391,12 +395,12 @@ __device__ __forceinline__ uint32_t half_of_bin(int bin) {
 __device__ __forceinline__ float value_of_bin(int bin) { return __uint_as_float(half_of_bin(bin) << 16); }
 
 // What lies outside the bins: NaN and -inf weigh nothing (0); a negative of 512
-// and more weighs nothing beside a largest logit well above (2); the rest is
-// for sample_any (1).
+// and more weighs nothing beside a largest logit well above (2); a positive one
+// is for sample_any (1).
 constexpr uint32_t kElsewhere = 1, kFarBelow = 2;
 __device__ __forceinline__ uint32_t outside(uint32_t bits) {
   if ((bits & 0x7FFFFFFFu) > 0x7F800000u || bits == 0xFF800000u) return 0;
-  return !(bits & 0x80000000u) || (bits & 0x7FFFFFFFu) >> 16 < (uint32_t)kLow ? kElsewhere : kFarBelow;
+  return !(bits & 0x80000000u) ? kElsewhere : kFarBelow;
 }
 // e^-60 of the largest weight: 2^42 times less than a unit for all of a row's
 // tokens together
@@ -534,11 +538,16 @@ __device__ __forceinline__ void gather_sums(Bins& s, u64& high, double& soft) {
 
 // bf16: one read of the row into the histogram, exponentials of the bins that
 // have tokens, the borders by one wave, and a second read for the token's index.
+constexpr int kSmall = 16;
 struct BinsBf16 {
   Bins b;
   uint32_t zeros, half, nth, top;
+  uint32_t small_n, mixed;  // nonzero logits below the bins; set if a border lies among them
+  uint16_t small[kSmall];
+  u64 small_m;              // their weight
   double conf, prob;
 };
+static_assert(sizeof(BinsBf16) <= 40960, "four workgroups a CU");
 template <int NT, int WAVES_PER_SIMD>
 __global__ __launch_bounds__(NT, WAVES_PER_SIMD) void sample_bf16_kernel(SampleRows r) {
   __shared__ union {
@@ -555,6 +564,8 @@ __global__ __launch_bounds__(NT, WAVES_PER_SIMD) void sample_bf16_kernel(SampleR
   if (threadIdx.x == 0) {
     s.zeros = 0;
     s.top = 0;
+    s.small_n = s.mixed = 0;
+    s.small_m = 0;
   }
   __syncthreads();
 
@@ -587,8 +598,15 @@ __global__ __launch_bounds__(NT, WAVES_PER_SIMD) void sample_bf16_kernel(SampleR
 #pragma unroll 1
         for (int j = 0; j < 8; ++j) {
           const uint32_t p = ((j < 4 ? j < 2 ? v[0] : v[1] : j < 6 ? v[2] : v[3]) >> (16 * (j & 1))) & 0xFFFFu;
-          if ((p & 0x7FFFu) == 0) atomicAdd(&s.zeros, 1u);
-          else if ((p & 0x7FFFu) - (uint32_t)kLow >= (uint32_t)kRange) flags |= outside(p << 16);
+          if ((p & 0x7FFFu) == 0) {
+            atomicAdd(&s.zeros, 1u);
+          } else if ((p & 0x7FFFu) < (uint32_t)kLow) {
+            const uint32_t at = atomicAdd(&s.small_n, 1u);
+            if (at < (uint32_t)kSmall) s.small[at] = (uint16_t)p;
+            else flags |= kElsewhere;
+          } else if ((p & 0x7FFFu) - (uint32_t)kLow >= (uint32_t)kRange) {
+            flags |= outside(p << 16);
+          }
         }
       }
     }
@@ -605,7 +623,7 @@ __global__ __launch_bounds__(NT, WAVES_PER_SIMD) void sample_bf16_kernel(SampleR
   if (flags) atomicOr(&s.b.flags, flags);
   __syncthreads();
   if (threadIdx.x == 0) {
-    s.b.count[kRange] = s.zeros;
+    s.b.count[kRange] = s.zeros + s.small_n;
     s.b.count[kValues] = 0;
   }
   float m = __uint_as_float(s.top << 16);
@@ -624,13 +642,24 @@ __global__ __launch_bounds__(NT, WAVES_PER_SIMD) void sample_bf16_kernel(SampleR
     __syncthreads();
     m = s.b.first < kValues ? value_of_bin(s.b.first) : -INFINITY;
   }
-  if (!by_bins(s.b.flags, m, set.scale)) {
+  const bool small_top = m == 0.f && s.small_n != 0;
+  if (small_top || !by_bins(s.b.flags, m, set.scale)) {
     __syncthreads();
     sample_any<bf16>(sh.any, r, row);
     return;
   }
   u64 high = 0;
   double soft = 0.0;
+  if (s.small_n) {
+    if (threadIdx.x < s.small_n) {
+      const double d = (double)__uint_as_float((uint32_t)s.small[threadIdx.x] << 16) - (double)m;
+      const double w = exp_down(s.b.table, d, set.scale);
+      atomicAdd(&s.small_m, units_of(w));
+      if (w >= set.min_p) high += units_of(w);
+      if (r.conf) soft += exp_down(s.b.table, d, kScaleOne);
+    }
+    __syncthreads();
+  }
 #pragma unroll 1
   for (int g = wave; g < kGroups; g += waves) {
     const int bin = g * 128 + 2 * lane;
@@ -642,10 +671,12 @@ __global__ __launch_bounds__(NT, WAVES_PER_SIMD) void sample_bf16_kernel(SampleR
       if (c[i]) {
         const double d = (double)value_of_bin(bin + i) - (double)m;
         const double w = exp_down(s.b.table, d, set.scale);
-        const u64 own = c[i] * units_of(w);
+        const uint32_t n = bin + i == kRange ? s.zeros : c[i];
+        const u64 own = n * units_of(w);
         mass += own;
         if (w >= set.min_p) high += own;
-        if (r.conf) soft += c[i] * exp_down(s.b.table, d, kScaleOne);
+        if (r.conf) soft += n * exp_down(s.b.table, d, kScaleOne);
+        if (bin + i == kRange) mass += s.small_m;
       }
     const u64 mt = wave_total(mass);
     const uint32_t ct = wave_total(c[0] + c[1]);
@@ -663,13 +694,16 @@ __global__ __launch_bounds__(NT, WAVES_PER_SIMD) void sample_bf16_kernel(SampleR
       valid += s.b.group_c[g];
     }
     const Draw d = draw_by(set, wave_total(all), high, wave_total(valid),
-                           [&](int cut, uint32_t want_c, u64 want_m) {
-                             return find_bin(s.b, cut != 0, want_c, want_m, [&](int bin) -> u64 {
-                               const uint32_t c = s.b.count[place_of(bin)];
-                               return c ? c * units_of(exp_down(s.b.table, (double)value_of_bin(bin) - (double)m, set.scale)) : 0;
+                           [&](int cut, uint32_t want_c, u64 want_m) -> Border {
+                             const Border f = find_bin(s.b, cut != 0, want_c, want_m, [&](int bin) -> u64 {
+                               const uint32_t c = bin == kRange ? s.zeros : s.b.count[place_of(bin)];
+                               const u64 own = c ? c * units_of(exp_down(s.b.table, (double)value_of_bin(bin) - (double)m, set.scale)) : 0;
+                               return bin == kRange ? own + s.small_m : own;
                              });
+                             return f.at == kRange && s.small_n != 0 ? Border{0, 0, 0, 0, 0} : f;
                            });
     if (lane == 0) {
+      s.mixed = d.at.in_c == 0;
       s.half = half_of_bin(d.at.at);
       s.nth = d.nth;
       s.prob = d.prob;
@@ -677,6 +711,11 @@ __global__ __launch_bounds__(NT, WAVES_PER_SIMD) void sample_bf16_kernel(SampleR
     }
   }
   __syncthreads();
+  if (s.mixed) {
+    __syncthreads();
+    sample_any<bf16>(sh.any, r, row);
+    return;
+  }
 
   // the nth token of that value: counted by round and wave in the counts' place,
   // then within a wave's pieces of one round
@@ -781,12 +820,12 @@ __global__ __launch_bounds__(kMaxThreads) void sample_f32_kernel(SampleRows r) {
   float m = -INFINITY;
   uint32_t flags = 0;
   auto zero = [](uint32_t bits) { return (bits << 1) == 0; };
-  auto in_bins = [&](uint32_t bits) { return zero(bits) || ((bits >> 16) & 0x7FFFu) - (uint32_t)kLow < (uint32_t)kRange; };
+  auto offset = [](uint32_t bits) { return (int)((bits >> 16) & 0x7FFFu) - kLow; };  // negative: the bin of zeros
   x.each_long([&](int, const u32x4& v) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       m = fmaxf(m, __uint_as_float(v[j]));
-      if (!in_bins(v[j])) flags |= outside(v[j]);
+      if (offset(v[j]) >= kRange) flags |= outside(v[j]);
     }
   });
   m = wave_max(m);
@@ -808,14 +847,14 @@ __global__ __launch_bounds__(kMaxThreads) void sample_f32_kernel(SampleRows r) {
     if (x.index(round, 0) >= r.n) return;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (!in_bins(v[j])) continue;
-      const int off = (int)((v[j] >> 16) & 0x7FFFu) - kLow;
-      const int bin = zero(v[j]) ? kRange : (int)(v[j] >> 31) * (kRange + 1) + off;  // its place
+      const int off = offset(v[j]);
+      if (off >= kRange) continue;
+      const int bin = off < 0 ? kRange : (int)(v[j] >> 31) * (kRange + 1) + off;  // its place
       const double w = weight(v[j]);
       const u64 units = units_of(w);
       atomicAdd(&s.b.count[bin], 1u);
       if (units) atomicAdd(&s.mass[bin], units);
-      if (w >= set.min_p) high += units;
+      if (set.min_p > 0.0 && w >= set.min_p) high += units;
       if (r.conf) soft += same_scale ? w : exp_down(s.b.table, (double)__uint_as_float(v[j]) - (double)m, kScaleOne);
     }
   });
@@ -841,6 +880,7 @@ __global__ __launch_bounds__(kMaxThreads) void sample_f32_kernel(SampleRows r) {
   }
   all = wave_total(all);
   valid = wave_total(valid);
+  if (!(set.min_p > 0.0)) high = all;
 
   // entry `at` of the list is the border's only token, or -1: list_n tokens of
   // the value `key`
@@ -867,8 +907,8 @@ __global__ __launch_bounds__(kMaxThreads) void sample_f32_kernel(SampleRows r) {
     x.each_long([&](int round, const u32x4& v) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (v[j] >> 16 == upper || (bin == kRange && zero(v[j]))) {
-          const uint32_t at = atomicAdd(&s.list_n, 1u), key = bin == kRange ? 0u : v[j];
+        if (bin == kRange ? offset(v[j]) < 0 : v[j] >> 16 == upper) {
+          const uint32_t at = atomicAdd(&s.list_n, 1u), key = zero(v[j]) ? 0u : v[j];
           atomicMin(&s.list_min, key);
           atomicMax(&s.list_max, key);
           if (at < kListed) {
@@ -885,7 +925,7 @@ __global__ __launch_bounds__(kMaxThreads) void sample_f32_kernel(SampleRows r) {
       __syncthreads();
       return f;
     }
-    if (n > kListed) return Border{0, 0, 0, 0, 0};  // not found this way
+    if (n > kListed || bin == kRange) return Border{0, 0, 0, 0, 0};  // not found this way
     const uint32_t turn = bin < kRange ? 255u : 0u;  // the largest value first
     const int t = threadIdx.x;
     const uint32_t mine = t < n ? s.list_key[t] : 0;

@@ -122,6 +122,38 @@ def test_values_at_the_ends(dt):
 
 
 @pytest.mark.parametrize("dt", [BF, F32])
+def test_logits_next_to_zero(dt):
+    """A few of them beside ordinary ones, many, the largest among them, and a border between them."""
+    n = 3001
+    g = torch.Generator().manual_seed(8)
+    tiny = torch.tensor([1e-10, -1e-12, 3e-9, -2e-38, 1e-30, 7e-9, -6e-9, 1e-20, -1e-20, 2e-39])
+    at = lambda count: torch.randperm(n, generator=g)[:count]
+    x = logits(8, n, F32, 9).clone()
+    x[0, at(10)] = tiny
+    x[1, at(20)] = tiny.repeat(2)
+    x[2] = -x[2].abs()
+    x[2, at(10)] = -tiny.abs()
+    x[2, at(5)] = 0.0
+    x[3] = -x[3].abs()
+    x[3, at(10)] = tiny
+    x[4] = -x[4].abs() - 1
+    x[4, at(2000)] = 0.0
+    x[4, at(10)] = tiny
+    x[5] = tiny[torch.randint(10, (n,), generator=g)]
+    x[5, at(1000)] = 0.0
+    x[6, at(1)] = 1e-10
+    x[6, at(800)] = -0.0
+    x[7, at(16)] = tiny[torch.randint(10, (16,), generator=g)]
+    x = x.to(dt)
+    rows = x.repeat(5, 1)
+    us = [u for u in (0.0, 0.2, 0.5, 0.9, 1.0 - 2.0 ** -53) for _ in range(8)]
+    check(rows, us, what="as they are")
+    check(rows, us, t=[0.8] * 40, k=[1500] * 40, p=[0.9] * 40, what="top-k and top-p")
+    check(rows, us, t=[3.0] * 40, m=[0.3] * 40, what="min-p")
+    check(rows, us, t=[50.0] * 40, k=[2010] * 40, what="all but equal weights, top-k")
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
 def test_settings_at_their_ends(dt):
     inf, nan = math.inf, math.nan
     x = logits(9, 1500, dt, 4)
