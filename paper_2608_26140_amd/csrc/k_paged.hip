@@ -710,9 +710,12 @@ __global__ __launch_bounds__(256, 2) void paged_attention_wide_kernel(PagedCache
 
 // fp32: 16 lanes share a key (elements lane % 16 + 16 i), a wave four keys at a
 // time, four such on their way; every 16 lanes keep a running softmax of their
-// own for the tile's four queries.  Bound by its chains of dependent instructions
-// (a sum over 16 lanes and two exponentials for a key and query): 5 rows of 3
-// requests over 403 keys, 8 heads of 32 on 4: 9 us of kernels and the join.
+// own for the tile's four queries, four keys of it at a time.  Bound by the
+// latency of a step (block id, rows, sums over 16 lanes): 5 rows of 3 requests
+// over 403 keys, 8 heads of 32 on 4: 11.7 us with the join, 17.4 with a softmax
+// step for each key and a join of the 16 streams by one thread an element; 16
+// requests over 4096 keys, heads of 128: 147 us.  Measured and no better: block
+// ids asked for a step ahead (151), pairs of elements by one load (155).
 constexpr int kQueriesF32 = 4;
 
 // The sum over the 16 lanes of a row, in each of them (moves in registers: by
@@ -732,13 +735,14 @@ __device__ __forceinline__ float row_sum(float v) {
 template <int N>  // elements of a head that a lane has, head_dim <= 16 N
 __global__ __launch_bounds__(256) void paged_attention_f32_kernel(PagedCache c, PagedQueries r, PagedPlan p) {
   constexpr int Q = kQueriesF32, U = 4;
-  __shared__ float s_out[16][128];
-  __shared__ float s_m[16], s_l[16];
+  static_assert(Q == 4, "a wave joins a query");
+  __shared__ float s_out[16][Q][16 * N];
+  __shared__ float s_m[Q][16], s_l[Q][16];
   Group gr;
   if (!group_of(c, p, gr)) return;
   const int ln = threadIdx.x & 15, str = threadIdx.x >> 4;  // 16 streams of keys
   const int rep = r.heads / c.kv_heads, nq = r.per_request * rep, q0 = gr.tile * Q, d = c.head_dim;
-  int klen[Q], longest = 0;
+  int klen[Q], longest = 0, shortest = 0x7FFFFFFF;
   float q[Q][N], m[Q], l[Q], acc[Q][N];
   const float scale = kLog2e / sqrtf((float)d);
 #pragma unroll
@@ -748,6 +752,7 @@ __global__ __launch_bounds__(256) void paged_attention_f32_kernel(PagedCache c, 
     const int64_t row = (int64_t)gr.b * r.per_request + i;
     klen[t] = real ? capped_len(c, r.key_len[row]) : 0;
     longest = max(longest, klen[t]);
+    if (real) shortest = min(shortest, klen[t]);
     const float* src = (const float*)r.q + row * r.q_ld + (int64_t)(gr.g * rep + (real ? q0 + t - i * rep : 0)) * d;
     m[t] = -INFINITY;
     l[t] = 0.f;
@@ -760,11 +765,11 @@ __global__ __launch_bounds__(256) void paged_attention_f32_kernel(PagedCache c, 
   int begin, end;
   share_of(longest, p.splits, gr.split, begin, end);
   const int32_t* table = c.tables + (int64_t)gr.b * c.table_ld;
-  for (int k0 = begin + str; k0 < end; k0 += 16 * U) {
+  for (int k0 = begin; k0 < end; k0 += 16 * U) {
     int slot[U];
-    float kv[U][N], vv[U][N];
+    float kv[U][N], vv[U][N], s[U][Q];
 #pragma unroll
-    for (int u = 0; u < U; ++u) slot[u] = k0 + 16 * u < end ? slot_of(c, table, k0 + 16 * u) : -1;
+    for (int u = 0; u < U; ++u) slot[u] = k0 + 16 * u + str < end ? slot_of(c, table, k0 + 16 * u + str) : -1;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int64_t off = (int64_t)max(slot[u], 0) * c.ld + gr.g * d;
@@ -779,51 +784,70 @@ __global__ __launch_bounds__(256) void paged_attention_f32_kernel(PagedCache c, 
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int t = 0; t < Q; ++t) {
-        float s = 0.f;
+        float x = 0.f;
 #pragma unroll
-        for (int e = 0; e < N; ++e) s += q[t][e] * kv[u][e];
-        s = row_sum(s);
-        if (k0 + 16 * u >= klen[t] || s == -INFINITY) continue;  // uniform over the 16 lanes
-        const float top = fmaxf(m[t], s);
-        const float f = m[t] == top ? 1.f : __builtin_amdgcn_exp2f(m[t] - top);
-        const float w = __builtin_amdgcn_exp2f(s - top);
-        l[t] = l[t] * f + w;
-        m[t] = top;
-#pragma unroll
-        for (int e = 0; e < N; ++e) acc[t][e] = acc[t][e] * f + w * vv[u][e];
+        for (int e = 0; e < N; ++e) x += q[t][e] * kv[u][e];
+        s[u][t] = row_sum(x);
       }
+    const bool whole = k0 + 16 * U <= shortest;  // for every query
+#pragma unroll
+    for (int t = 0; t < Q; ++t) {
+      float top = m[t];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (!whole) s[u][t] = k0 + 16 * u + str < klen[t] ? s[u][t] : -INFINITY;
+        top = fmaxf(top, s[u][t]);
+      }
+      const float f = m[t] == top ? 1.f : __builtin_amdgcn_exp2f(m[t] - top), from = top == -INFINITY ? 0.f : top;
+      m[t] = top;
+      l[t] *= f;
+#pragma unroll
+      for (int e = 0; e < N; ++e) acc[t][e] *= f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float w = __builtin_amdgcn_exp2f(s[u][t] - from);
+        l[t] += w;
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[t][e] += w * (whole || s[u][t] != -INFINITY ? vv[u][e] : 0.f);
+      }
+    }
   }
 #pragma unroll
   for (int t = 0; t < Q; ++t) {
     if (ln == 0) {
-      s_m[str] = m[t];
-      s_l[str] = l[t];
+      s_m[t][str] = m[t];
+      s_l[t][str] = l[t];
     }
 #pragma unroll
-    for (int e = 0; e < N; ++e) s_out[str][ln + 16 * e] = acc[t][e];
-    __syncthreads();
-    if (q0 + t < nq && (int)threadIdx.x < d) {
-      float top = s_m[0];
-      for (int w = 1; w < 16; ++w) top = fmaxf(top, s_m[w]);
-      const float from = top == -INFINITY ? 0.f : top;
-      float total = 0.f, o = 0.f;
-      for (int w = 0; w < 16; ++w) {
-        const float f = s_m[w] == top ? 1.f : __builtin_amdgcn_exp2f(s_m[w] - from);
-        total += s_l[w] * f;
-        if (s_l[w] != 0.f) o += s_out[w][threadIdx.x] * f;
-      }
-      const int i = (q0 + t) / rep, h = gr.g * rep + q0 + t - i * rep;
-      const int64_t row = (int64_t)gr.b * r.per_request + i;
-      if (p.splits == 1) {
-        ((float*)r.out)[row * r.out_ld + (int64_t)h * d + threadIdx.x] = total == 0.f ? 0.f : o / total;
-        if (r.lse && threadIdx.x == 0) r.lse[row * r.heads + h] = (from + __builtin_amdgcn_logf(total)) * kLn2;
-      } else {
-        const int64_t at = ((int64_t)gr.split * c.batch * r.per_request + row) * r.heads + h;
-        p.part[at * d + threadIdx.x] = o;
-        if (threadIdx.x == 0) p.stats[at] = make_float2(top, total);
-      }
+    for (int e = 0; e < N; ++e) s_out[str][t][ln + 16 * e] = acc[t][e];
+  }
+  __syncthreads();
+  // wave t joins the 16 streams of query t
+  const int t = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  if (q0 + t >= nq) return;
+  const float own = s_m[t][ln], own_l = s_l[t][ln];
+  float top = own;
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+  const float from = top == -INFINITY ? 0.f : top;
+  const float f = own_l == 0.f ? 0.f : own == top ? 1.f : __builtin_amdgcn_exp2f(own - from);
+  const float total = row_sum(own_l * f);
+  const int i = (q0 + t) / rep, h = gr.g * rep + q0 + t - i * rep;
+  const int64_t row = (int64_t)gr.b * r.per_request + i;
+  const int64_t at = ((int64_t)gr.split * c.batch * r.per_request + row) * r.heads + h;
+  for (int e = lane; e < d; e += 64) {
+    float o = 0.f;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+      const float fw = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(f), w));
+      if (fw != 0.f) o += s_out[w][t][e] * fw;
     }
-    __syncthreads();
+    if (p.splits == 1) ((float*)r.out)[row * r.out_ld + (int64_t)h * d + e] = total == 0.f ? 0.f : o / total;
+    else p.part[at * d + e] = o;
+  }
+  if (lane == 0) {
+    if (p.splits > 1) p.stats[at] = make_float2(top, total);
+    else if (r.lse) r.lse[row * r.heads + h] = (from + __builtin_amdgcn_logf(total)) * kLn2;
   }
 }
 
@@ -986,8 +1010,8 @@ hipError_t launch_paged_attention(acache_dtype dt, const PagedCache& c, const Pa
   const dim3 grid((unsigned)((keys + 7) / 8 * 8 * p.tiles));
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, c, r, p); };
   if (dt == ACACHE_F32) {
-    // 16 requests of 5 rows, 8 heads of 32 on 4, over 4096 keys: 60 us, 107 with the
-    // elements of a head of 128; heads of 64: 84, 119
+    // 16 requests of 5 rows, 8 heads of 32 on 4, over 4096 keys: 53 us, 92 with the
+    // elements of a head of 128; heads of 64: 79, 104
     if (c.head_dim <= 32) go(paged_attention_f32_kernel<2>);
     else if (c.head_dim <= 64) go(paged_attention_f32_kernel<4>);
     else go(paged_attention_f32_kernel<8>);
