@@ -637,7 +637,8 @@ acache_status acache_paged_append(const acache_dims* dims, const acache_paged_ca
  * tables' capacity); it sets how the keys are split over workgroups and nothing
  * else.  ws is optional: with acache_paged_workspace_size() bytes calls with
  * few rows split the keys (fp32 partials, joined in a fixed order); with less,
- * in fewer parts or none.  rows and batch * H_kv * (rows_per_request * H / H_kv / 16,
+ * in fewer parts or none; calls that may overlap need workspaces of their own.
+ * rows and batch * H_kv * (rows_per_request * H / H_kv / 16,
  * f32 4, rounded up) are below 2^24 (ACACHE_ERR_UNSUPPORTED otherwise).  rows == 0:
  * no-op. */
 acache_status acache_paged_attention(const acache_dims* dims, const acache_paged_cache* cache, int32_t rows_per_request,

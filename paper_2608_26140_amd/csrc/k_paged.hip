@@ -944,8 +944,8 @@ hipError_t launch_paged_append(acache_dtype dt, const PagedCache& c, const Appen
   const double l2b = log2((double)rope_base);
   const int half = c.head_dim / 2, heads = (r.q ? r.heads : 0) + 2 * c.kv_heads;
   // Below 1024 rows a row's items are spread over workgroups, each with all of its
-  // angles: 512 rows of 28 + 8 heads 4.3 us, 7.7 with several rows to a workgroup;
-  // from there on one takes them all: 1024 rows 6.3, spread 7.2, 8192 rows 30.5, 40.
+  // angles: 128 rows of 32 + 64 heads 3.4 us, 4.1 with one; from there on one takes
+  // them all: 4096 rows 35.7, spread 39.7, 8192 of 28 + 8 heads 30.5, 40.
   auto go = [&](auto kernel, int v) {
     const int parts = r.n >= 1024 ? 1 : std::min(64, (heads * (half / v) + 255) / 256);
     hipLaunchKernelGGL(kernel, dim3(r.n, parts), dim3(256), (size_t)half * sizeof(float2), s, c, r, l2b);

@@ -538,6 +538,8 @@ __device__ __forceinline__ void gather_sums(Bins& s, u64& high, double& soft) {
 
 // bf16: one read of the row into the histogram, exponentials of the bins that
 // have tokens, the borders by one wave, and a second read for the token's index.
+// Bound by the LDS atomics of the first read, one a logit: a row of 126464 21.9 us,
+// 1024 rows 78 us.
 constexpr int kSmall = 16;
 struct BinsBf16 {
   Bins b;
@@ -790,7 +792,9 @@ __global__ __launch_bounds__(NT, WAVES_PER_SIMD) void sample_bf16_kernel(SampleR
 // fp32: a read for the largest logit, one for the bins' counts and weights, and
 // one for each border whose bin has more than one token, or that is drawn from:
 // the bin's tokens are listed, told apart by their next eight bits, and those of
-// one such value by comparing them all.
+// one such value by comparing them all.  Bound by the second read, some 70
+// instructions a logit (the 64-bit exponential, two LDS atomics): 67 rows of 50021
+// 44 us.
 constexpr int kListed = 1024;
 struct BinsF32 {
   Bins b;
@@ -1020,10 +1024,10 @@ __global__ __launch_bounds__(kMaxThreads) void sample_f32_kernel(SampleRows r) {
 }  // namespace
 
 hipError_t launch_sample_commit(acache_dtype dt, const SampleRows& r, int rows, hipStream_t s) {
-  // bf16: with a row for every CU at most, 1024 threads for each (one row of
-  // 126464: 21.6 us, 23.6 with 512); with more, four rows side by side on a CU,
-  // 512 threads and 64 registers each, so that one row's search runs behind the
-  // others' reads (1024 rows: 84 us; two rows of 1024 threads a CU 86, one 104)
+  // bf16: with a row for every CU at most, 1024 threads for each (rows of 126464:
+  // one 21.4 us, 24.0 with 512; 256 26.3, 30.2); with more, four rows side by side
+  // on a CU, 512 threads and 64 registers each, so that one row's search runs
+  // behind the others' reads (512 rows 44.6, 50.9 with 1024 threads; 1024 77, 99)
   if (dt == ACACHE_F32) hipLaunchKernelGGL(sample_f32_kernel, dim3(rows), dim3(kMaxThreads), 0, s, r);
   else if (rows <= 256) hipLaunchKernelGGL((sample_bf16_kernel<kMaxThreads, 4>), dim3(rows), dim3(kMaxThreads), 0, s, r);
   else hipLaunchKernelGGL((sample_bf16_kernel<512, 8>), dim3(rows), dim3(512), 0, s, r);
