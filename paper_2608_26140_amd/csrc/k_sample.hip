@@ -890,6 +890,7 @@ __global__ __launch_bounds__(kMaxThreads) void sample_f32_kernel(SampleRows r) {
   // the value `key`
   int only = -1;
   const Draw d = draw_by(set, all, high, valid, [&](int cut, uint32_t want_c, u64 want_m) -> Border {
+    __syncthreads();  // every wave has read the last cut's border, its list and its counts
     if (wave == 0) {
       const Border f = find_bin(s.b, cut != 0, want_c, want_m, [&](int bin) { return s.mass[place_of(bin)]; });
       if (lane == 0) s.border = f;
@@ -971,7 +972,6 @@ __global__ __launch_bounds__(kMaxThreads) void sample_f32_kernel(SampleRows r) {
     __syncthreads();
     f = s.border;
     only = f.at;
-    __syncthreads();
     return f;
   });
   if (d.at.in_c == 0) {
