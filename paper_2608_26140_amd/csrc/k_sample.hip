@@ -395,16 +395,18 @@ __device__ __forceinline__ uint32_t half_of_bin(int bin) {
 __device__ __forceinline__ float value_of_bin(int bin) { return __uint_as_float(half_of_bin(bin) << 16); }
 
 // What lies outside the bins: NaN and -inf weigh nothing (0); a negative of 512
-// and more weighs nothing beside a largest logit well above (2); a positive one
-// is for sample_any (1).
+// and more weighs nothing beside a largest logit well above (2, see by_bins); a
+// positive one is for sample_any (1).
 constexpr uint32_t kElsewhere = 1, kFarBelow = 2;
 __device__ __forceinline__ uint32_t outside(uint32_t bits) {
   if ((bits & 0x7FFFFFFFu) > 0x7F800000u || bits == 0xFF800000u) return 0;
   return !(bits & 0x80000000u) ? kElsewhere : kFarBelow;
 }
-// e^-60 of the largest weight: 2^42 times less than a unit for all of a row's
-// tokens together
-__device__ __forceinline__ bool by_bins(uint32_t flags, float m, double scale) {
+// What is left out may weigh e^-60 of the largest at most, so that a whole row of
+// 2^19 such tokens is 2^23 times less than a unit: at the temperature drawn with
+// and, where the confidence is asked for, at 1, whichever makes more of them.
+__device__ __forceinline__ bool by_bins(uint32_t flags, float m, double scale, bool conf) {
+  if (conf) scale = fmin(scale, kScaleOne);
   return !(flags & kElsewhere) && m > -512.f && (!(flags & kFarBelow) || ((double)m + 512.0) * scale > 60.0 * kScaleOne);
 }
 
@@ -645,7 +647,7 @@ __global__ __launch_bounds__(NT, WAVES_PER_SIMD) void sample_bf16_kernel(SampleR
     m = s.b.first < kValues ? value_of_bin(s.b.first) : -INFINITY;
   }
   const bool small_top = m == 0.f && s.small_n != 0;
-  if (small_top || !by_bins(s.b.flags, m, set.scale)) {
+  if (small_top || !by_bins(s.b.flags, m, set.scale, r.conf != nullptr)) {
     __syncthreads();
     sample_any<bf16>(sh.any, r, row);
     return;
@@ -838,7 +840,7 @@ __global__ __launch_bounds__(kMaxThreads) void sample_f32_kernel(SampleRows r) {
   if (flags) atomicOr(&s.b.flags, flags);
   __syncthreads();
   for (int w = 0; w < waves; ++w) m = fmaxf(m, s.b.part_f[w]);
-  if (!by_bins(s.b.flags, m, set.scale)) {
+  if (!by_bins(s.b.flags, m, set.scale, r.conf != nullptr)) {
     __syncthreads();
     sample_any<float>(sh.any, r, row);
     return;
