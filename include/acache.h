@@ -587,7 +587,8 @@ size_t acache_quant_layer_workspace_size(const acache_dims* dims, int32_t max_ro
  * pools.  A position that is negative or past the table, or whose entry is
  * outside [0, n_blocks), has no slot: nothing is stored there and it reads as a
  * key and a value of zeros.  Several requests may name one block (a shared
- * prefix).  Slots are addressed with 64-bit offsets. */
+ * prefix).  Slots are addressed with 64-bit offsets, what lies in a row with 32
+ * bits: (H + 2 H_kv) * head_dim < 2^31 (ACACHE_ERR_UNSUPPORTED otherwise). */
 typedef struct {
   void* k;               /* [n_blocks * block, ld] of dims->dtype, a slot's row H_kv heads of head_dim (K after rotation) */
   void* v;
@@ -638,16 +639,16 @@ acache_status acache_paged_append(const acache_dims* dims, const acache_paged_ca
  * else.  ws is optional: with acache_paged_workspace_size() bytes calls with
  * few rows split the keys (fp32 partials, joined in a fixed order); with less,
  * in fewer parts or none; calls that may overlap need workspaces of their own.
- * rows and batch * H_kv * (rows_per_request * H / H_kv / 16,
- * f32 4, rounded up) are below 2^24 (ACACHE_ERR_UNSUPPORTED otherwise).  rows == 0:
- * no-op. */
+ * rows are below 2^24, and so is batch * H_kv, rounded up to a multiple of 8, times
+ * the tiles that a KV head's rows_per_request * H / H_kv queries make (of 16 at
+ * least, f32 4); more is ACACHE_ERR_UNSUPPORTED.  rows == 0: no-op. */
 acache_status acache_paged_attention(const acache_dims* dims, const acache_paged_cache* cache, int32_t rows_per_request,
                                      const void* q, int64_t q_ld, const int32_t* key_len, int64_t max_len, void* out,
                                      int64_t out_ld, float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* Workspace bytes with which acache_paged_attention splits the keys as it
- * likes (its pointers are not looked at).  0 for invalid dims or cache, 256 at
- * least otherwise. */
+ * likes (its pointers are not looked at).  0 for invalid dims or cache and for more
+ * rows than a call takes, 256 at least otherwise. */
 size_t acache_paged_workspace_size(const acache_dims* dims, const acache_paged_cache* cache, int32_t rows_per_request,
                                    int64_t max_len);
 

@@ -844,7 +844,7 @@ def acache_paged_append(dims: Dims, cache: PagedCache, k: torch.Tensor, v: torch
 def acache_paged_workspace_size(dims: Dims, cache: PagedCache, rows_per_request: int, max_len: int = 0) -> int:
     n = lib.acache_paged_workspace_size(ctypes.byref(dims), cache.ref, rows_per_request, max_len)
     if n == 0:
-        raise AcacheError("acache_paged_workspace_size", 2, "invalid dims or cache")
+        raise AcacheError("acache_paged_workspace_size", 2, "invalid dims or cache, or too many rows")
     return n
 
 

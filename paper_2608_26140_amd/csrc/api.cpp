@@ -1167,6 +1167,8 @@ acache_status check_paged(const acache_dims* d, const acache_paged_cache* c, int
         ACACHE_ERR_UNSUPPORTED);
   // a launch has less than 2^24 workgroups of 256 threads
   CHECK((int64_t)c->batch * rows_per_request < 1 << 24, ACACHE_ERR_UNSUPPORTED);
+  // offsets within a row are of 32 bits
+  CHECK(((int64_t)d->n_heads + 2 * (int64_t)d->n_kv_heads) * d->head_dim < k31, ACACHE_ERR_UNSUPPORTED);
   out = PagedCache{c->k, c->v, c->ld, (int)c->n_blocks, c->block, d->n_kv_heads, d->head_dim, c->tables, c->table_ld,
                    c->batch, c->max_blocks};
   return ACACHE_OK;
@@ -1226,7 +1228,7 @@ acache_status acache_paged_attention(const acache_dims* dims, const acache_paged
           ACACHE_ERR_ALIGN);
   CHECK(!ws || aligned16(ws), ACACHE_ERR_ALIGN);
   const PagedPlan plan = plan_paged(dims, c, rows_per_request, max_len, ws ? ws_bytes : 0);
-  CHECK((int64_t)c.batch * c.kv_heads * plan.splits * plan.tiles < (1 << 24) - 8 * (int64_t)plan.tiles, ACACHE_ERR_UNSUPPORTED);
+  CHECK(plan.splits > 0, ACACHE_ERR_UNSUPPORTED);
   const PagedQueries r = {q, q_ld, out, out_ld, lse, key_len, rows_per_request, dims->n_heads};
   LAUNCH_T(ACACHE_K_ATTENTION, stream, launch_paged_attention(dims->dtype, c, r, plan, ws, stream));
   return ACACHE_OK;
@@ -1237,7 +1239,8 @@ size_t acache_paged_workspace_size(const acache_dims* dims, const acache_paged_c
   PagedCache c;
   if (check_paged(dims, cache, rows_per_request, c) != ACACHE_OK) return 0;
   if (c.batch == 0 || rows_per_request == 0) return kAlign;
-  return std::max(kAlign, align_up(plan_paged(dims, c, rows_per_request, max_len, SIZE_MAX).ws_bytes));
+  const PagedPlan plan = plan_paged(dims, c, rows_per_request, max_len, SIZE_MAX);
+  return plan.splits == 0 ? 0 : std::max(kAlign, align_up(plan.ws_bytes));
 }
 
 acache_status acache_paged_attention_schedule(const acache_dims* dims, const acache_paged_cache* cache,
@@ -1246,7 +1249,10 @@ acache_status acache_paged_attention_schedule(const acache_dims* dims, const aca
   acache_status st = check_paged(dims, cache, rows_per_request, c);
   if (st != ACACHE_OK) return st;
   CHECK(splits, ACACHE_ERR_NULL);
-  *splits = c.batch == 0 || rows_per_request == 0 ? 0 : plan_paged(dims, c, rows_per_request, max_len, ws_bytes).splits;
+  *splits = 0;
+  if (c.batch == 0 || rows_per_request == 0) return ACACHE_OK;
+  *splits = plan_paged(dims, c, rows_per_request, max_len, ws_bytes).splits;
+  CHECK(*splits > 0, ACACHE_ERR_UNSUPPORTED);
   return ACACHE_OK;
 }
 

@@ -202,7 +202,8 @@ struct PagedQueries {
   int per_request, heads;
 };
 // tile: queries of a KV head that a workgroup takes; splits: of the keys, their
-// partials in ws_bytes of workspace (part [splits][pairs][head_dim], stats).
+// partials in ws_bytes of workspace (part [splits][pairs][head_dim], stats); 0:
+// more workgroups than a launch has.
 struct PagedPlan {
   int tile, tiles, splits;
   size_t ws_bytes;

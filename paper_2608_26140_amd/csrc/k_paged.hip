@@ -926,13 +926,17 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedCache c, PagedQue
 // Blocks are of whole runs of 16 slots, 16 rows of which lie within 2^31 bytes.
 bool in_runs(const PagedCache& c) { return c.block % 16 == 0 && c.ld < 1 << 26; }
 
+// Shares of the keys of all requests and KV heads, in whole rounds of the XCDs
+// (group_of): each takes a workgroup for every query tile.
+int64_t paged_groups(const PagedCache& c, int64_t splits) { return ((int64_t)c.batch * c.kv_heads * splits + 7) / 8 * 8; }
+
 // Tiles of 16 for up to 16 queries: 7 of each of 4 KV heads of 8 requests over 8192
 // keys 31.3 us, 33.7 with tiles of 32; 28 of each 47.9, 37.1.
 // Tiles of 128 from 193 queries on, where both of a KV head's first two are more
 // than half full: 4 x 32 rows of 28 heads on 4 (224 queries) over 5120 keys 28 us,
 // 32 with tiles of 32; 4 x 256 rows (1792) over 4096 keys 98, 122; but 160
 // queries of one KV head over 3000 keys 15.3, 13.4.
-int tile_queries(int queries, bool f32, bool runs) {
+int tile_queries(int64_t queries, bool f32, bool runs) {
   if (f32) return kQueriesF32;
   if (runs && queries > 192) return kWideQueries;
   return queries <= 16 ? 16 : 32;
@@ -959,16 +963,19 @@ hipError_t launch_paged_append(acache_dtype dt, const PagedCache& c, const Appen
 PagedPlan plan_paged_attention(acache_dtype dt, const PagedCache& c, int per_request, int heads, int64_t max_len,
                                size_t ws_bytes) {
   PagedPlan p = {};
-  const int queries = per_request * (heads / c.kv_heads);
+  const int64_t queries = (int64_t)per_request * (heads / c.kv_heads);
   p.tile = tile_queries(queries, dt == ACACHE_F32, in_runs(c));
-  p.tiles = (queries + p.tile - 1) / p.tile;
-  const int64_t groups = (int64_t)c.batch * c.kv_heads * p.tiles;
+  const int64_t tiles = (queries + p.tile - 1) / p.tile;
+  const int64_t groups = (int64_t)c.batch * c.kv_heads * tiles;
   const int64_t pairs = (int64_t)c.batch * per_request * heads;
   const size_t each = (size_t)pairs * (c.head_dim + 2) * sizeof(float);
   // a launch has less than 2^24 workgroups of 256 threads
   constexpr int64_t kMost = 1 << 24;
+  auto fits = [&](int64_t splits) { return paged_groups(c, splits) * tiles < kMost; };
+  if (!fits(1)) return p;
+  p.tiles = (int)tiles;
   const int64_t most = pairs >= kMost ? 1
-                                      : std::min<int64_t>({(max_len + 127) / 128, kMaxSplits, (kMost - 8) / groups,
+                                      : std::min<int64_t>({(max_len + 127) / 128, kMaxSplits,
                                                            (int64_t)(ws_bytes / std::max<size_t>(each, 1))});
   // The split with the least estimated time, in us.  Workgroups run two a CU, in
   // rounds; one takes a step for every 128 keys.  A step is the longest of a
@@ -983,7 +990,7 @@ PagedPlan plan_paged_attention(acache_dtype dt, const PagedCache& c, int per_req
   const double work = f32 ? 1.5 : p.tile == kWideQueries ? 2.8 : p.tile == 32 ? 1.05 : 0.6;
   int64_t splits = 1;
   double best = 1e30;
-  for (int64_t s = 1; s <= std::max<int64_t>(most, 1); ++s) {
+  for (int64_t s = 1; s <= std::max<int64_t>(most, 1) && fits(s); ++s) {
     const int64_t n = groups * s, running = std::min<int64_t>(n, 512);
     const double read = running * 256.0 * c.head_dim * (f32 ? 4 : 2) / 6e6 / p.tiles;
     const double step = std::max({chain + 0.35 * read, read, work * (double)((running + 255) / 256)});
@@ -995,7 +1002,7 @@ PagedPlan plan_paged_attention(acache_dtype dt, const PagedCache& c, int per_req
       splits = s;
     }
   }
-  p.splits = (int)std::max<int64_t>(splits, 1);
+  p.splits = (int)splits;
   p.ws_bytes = p.splits > 1 ? p.splits * each : 0;
   return p;
 }
@@ -1006,8 +1013,7 @@ hipError_t launch_paged_attention(acache_dtype dt, const PagedCache& c, const Pa
   const int64_t pairs = (int64_t)c.batch * r.per_request * r.heads;
   p.part = (float*)ws;
   p.stats = (float2*)(p.part + pairs * p.splits * c.head_dim);
-  const int64_t keys = (int64_t)c.batch * c.kv_heads * p.splits;
-  const dim3 grid((unsigned)((keys + 7) / 8 * 8 * p.tiles));
+  const dim3 grid((unsigned)(paged_groups(c, p.splits) * p.tiles));
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, c, r, p); };
   if (dt == ACACHE_F32) {
     // 16 requests of 5 rows, 8 heads of 32 on 4, over 4096 keys: 53 us, 92 with the
