@@ -441,11 +441,11 @@ class Sampling:
                  generator: Optional[torch.Generator] = None):
         n = batch.B * block_len
 
-        def rows(v, dtype):
-            t = torch.as_tensor(v, dtype=dtype, device=batch.device)
+        def rows(v, dtype):  # laid out on the host: the copy is done when it returns, for every stream
+            t = torch.as_tensor(v, dtype=dtype, device="cpu")
             if t.dim() > 1 or (t.dim() == 1 and t.numel() != batch.B):
                 raise ValueError("a setting is one number, or one for each request")
-            return t.expand(batch.B).repeat_interleave(block_len).contiguous()
+            return t.expand(batch.B).repeat_interleave(block_len).to(batch.device)
         self.settings = dict(temperature=rows(temperature, torch.float32), top_k=rows(top_k, torch.int32),
                              top_p=rows(top_p, torch.float32), min_p=rows(min_p, torch.float32))
         self.u = torch.empty(n, dtype=torch.float64, device=batch.device)
