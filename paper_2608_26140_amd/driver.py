@@ -439,8 +439,6 @@ class Sampling:
 
     def __init__(self, batch: AffixBatch, block_len: int, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
                  generator: Optional[torch.Generator] = None):
-        n = batch.B * block_len
-
         def rows(v, dtype):  # laid out on the host: the copy is done when it returns, for every stream
             t = torch.as_tensor(v, dtype=dtype, device="cpu")
             if t.dim() > 1 or (t.dim() == 1 and t.numel() != batch.B):
@@ -448,14 +446,14 @@ class Sampling:
             return t.expand(batch.B).repeat_interleave(block_len).to(batch.device)
         self.settings = dict(temperature=rows(temperature, torch.float32), top_k=rows(top_k, torch.int32),
                              top_p=rows(top_p, torch.float32), min_p=rows(min_p, torch.float32))
-        self.u = torch.empty(n, dtype=torch.float64, device=batch.device)
         self.generator = generator
 
     def commit(self, logits: torch.Tensor, stream=None, **to) -> torch.Tensor:
-        """acache_argmax_commit's call, drawn."""
+        """acache_argmax_commit's call, drawn with numbers of its own."""
         with _on(stream):
-            self.u.uniform_(generator=self.generator)
-        return A.acache_sample_commit(logits, self.u, **self.settings, **to, stream=stream)
+            u = torch.empty(logits.shape[0], dtype=torch.float64, device=logits.device)
+            u.uniform_(generator=self.generator)
+        return A.acache_sample_commit(logits, u, **self.settings, **to, stream=stream)
 
 
 def _commit(logits: torch.Tensor, sampling: Optional[Sampling], stream=None, **to):
