@@ -453,6 +453,8 @@ class Sampling:
         with _on(stream):
             u = torch.empty(logits.shape[0], dtype=torch.float64, device=logits.device)
             u.uniform_(generator=self.generator)
+            for t in self.settings.values():  # their memory is kept until this stream has read them
+                t.record_stream(torch.cuda.current_stream())
         return A.acache_sample_commit(logits, u, **self.settings, **to, stream=stream)
 
 

@@ -1,4 +1,5 @@
-"""Drawn tokens on a stream of their own."""
+"""Drawn tokens on a stream of their own: the settings are there when another stream reads
+them and stay until it has, and every commit has numbers of its own."""
 
 import pytest
 import torch
@@ -45,6 +46,21 @@ def test_settings_are_there_when_another_stream_reads_them():
     got = sampling.commit(logits, stream=side)
     side.synchronize()
     assert torch.equal(got, want)
+
+
+def test_settings_stay_until_another_stream_has_read_them():
+    batch, logits, want = setup()
+    side, generator = torch.cuda.Stream(), seeded(5)
+    sampling = D.Sampling(batch, BLOCK, **SETTINGS, generator=generator)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+    got = sampling.commit(logits, stream=side)
+    del sampling
+    after = scrap(batch)
+    torch.cuda.current_stream().synchronize()
+    side.synchronize()
+    assert torch.equal(got, want) and all((t == 7).all() for t in after)
 
 
 def test_numbers_are_a_commits_own(monkeypatch):
