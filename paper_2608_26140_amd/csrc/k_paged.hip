@@ -495,7 +495,7 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedCache c, P
 // Bound by its work: per tile and wave 32 products of 32 cycles, 32 exponentials
 // of 16 and some 200 other vector instructions, about half of what 32 queries
 // with keys of their own take (paged_attention_kernel): 4 x 256 rows of 28 heads
-// over 4096 keys 98 us, 0.61 PFLOP/s.
+// over 4096 keys 88 us, 0.68 PFLOP/s.
 typedef __attribute__((__vector_size__(4 * sizeof(int16_t)))) int16_t i16x4;
 __device__ __forceinline__ i16x4 read_turned(const char* lds) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)lds);
@@ -712,10 +712,11 @@ __global__ __launch_bounds__(256, 2) void paged_attention_wide_kernel(PagedCache
 // time, four such on their way; every 16 lanes keep a running softmax of their
 // own for the tile's four queries, four keys of it at a time.  Bound by the
 // latency of a step (block id, rows, sums over 16 lanes): 5 rows of 3 requests
-// over 403 keys, 8 heads of 32 on 4: 11.7 us with the join, 17.4 with a softmax
-// step for each key and a join of the 16 streams by one thread an element; 16
-// requests over 4096 keys, heads of 128: 147 us.  Measured and no better: block
-// ids asked for a step ahead (151), pairs of elements by one load (155).
+// over 403 keys, 4 heads of 32 on 2: 11.9 us with the join, 17.4 with a softmax
+// step for each key and a join of the 16 streams by one thread an element; 5 rows
+// of each of 16 requests over 4096 keys, 8 heads of 128 on 4: 148 us, three times
+// what the bytes take.  Measured there and no better: block ids asked for a step ahead (151),
+// pairs of elements by one load (155).
 constexpr int kQueriesF32 = 4;
 
 // The sum over the 16 lanes of a row, in each of them (moves in registers: by
@@ -933,9 +934,9 @@ int64_t paged_groups(const PagedCache& c, int64_t splits) { return ((int64_t)c.b
 // Tiles of 16 for up to 16 queries: 7 of each of 4 KV heads of 8 requests over 8192
 // keys 31.3 us, 33.7 with tiles of 32; 28 of each 47.9, 37.1.
 // Tiles of 128 from 193 queries on, where both of a KV head's first two are more
-// than half full: 4 x 32 rows of 28 heads on 4 (224 queries) over 5120 keys 28 us,
-// 32 with tiles of 32; 4 x 256 rows (1792) over 4096 keys 98, 122; but 160
-// queries of one KV head over 3000 keys 15.3, 13.4.
+// than half full: 4 x 32 rows of 28 heads on 4 (224 queries) over 5120 keys 27.4 us,
+// 31.5 with tiles of 32; 4 x 64 rows 40.3, 52.2; 4 x 256 rows (1792) over 4096 keys
+// 88, 113; but 160 queries of one KV head over 3000 keys 11.8, 11.1.
 int tile_queries(int64_t queries, bool f32, bool runs) {
   if (f32) return kQueriesF32;
   if (runs && queries > 192) return kWideQueries;

@@ -20,10 +20,12 @@
 // among the smallest ones when they are not all zeros, bf16 rows with more than
 // kSmall nonzero ones of these, and fp32 rows with more than 1024 tokens of
 // several values in a border's bin go by sample_any, which refines a histogram
-// over the logits' order keys and reads the row anew for each step (a call of
-// 1024 rows of 126464 takes 720 us with one such row, 77 without; of normally
-// distributed logits some 10^-9 are nonzero and below 2^-27, which is why these
-// have a place of their own).
+// over the logits' order keys and reads the row anew for each step.  A call of 1024
+// bf16 rows of 126464 takes 720 to 870 us with one such row, 79 without, one of 67
+// fp32 rows of 50021 108 and 44.  Of normally distributed logits some 10^-9 are
+// nonzero and below 2^-27, which is why these have a place of their own; fp32 logits
+// far from zero crowd a bin (67 rows of 126464 of spread 2.5: 93 us around 0, 100
+// around 5, 380 around 10, 430 around 20).
 #include "device.h"
 #include "internal.h"
 
@@ -540,8 +542,11 @@ __device__ __forceinline__ void gather_sums(Bins& s, u64& high, double& soft) {
 
 // bf16: one read of the row into the histogram, exponentials of the bins that
 // have tokens, the borders by one wave, and a second read for the token's index.
-// Bound by the LDS atomics of the first read, one a logit: a row of 126464 21.9 us,
-// 1024 rows 78 us.
+// Bound by its vector instructions, 14 a logit: with 1024 rows (78 us) they take 75%
+// of the SIMDs' cycles at four each, and the LDS works in 44% of a CU's (28% are
+// bank conflicts of the atomics, one a logit); a row of 126464, 21.8 us, on one CU:
+// 51% and 30%.  What is outside the bins, masked logits among it, adds to one place:
+// 1024 rows with 90% of -inf or of the type's lowest value take 410 us.
 constexpr int kSmall = 16;
 struct BinsBf16 {
   Bins b;
@@ -794,9 +799,9 @@ __global__ __launch_bounds__(NT, WAVES_PER_SIMD) void sample_bf16_kernel(SampleR
 // fp32: a read for the largest logit, one for the bins' counts and weights, and
 // one for each border whose bin has more than one token, or that is drawn from:
 // the bin's tokens are listed, told apart by their next eight bits, and those of
-// one such value by comparing them all.  Bound by the second read, some 70
-// instructions a logit (the 64-bit exponential, two LDS atomics): 67 rows of 50021
-// 44 us.
+// one such value by comparing them all.  Bound by the second read: all in all 96
+// vector instructions a logit (the 64-bit exponential), at four cycles each 75% of
+// the SIMDs' on the CUs that have a row; the LDS works in 26%.  67 rows of 50021 44 us.
 constexpr int kListed = 1024;
 struct BinsF32 {
   Bins b;
